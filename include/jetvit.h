@@ -264,6 +264,83 @@ jv_status jv_full_attn_fwd(const jv_attn_desc *desc, const void *q, const void *
                            const void *v, void *o, float scale, void *hip_stream);
 
 /* ---------------------------------------------------------------------------
+ * Differential attention: the difference of two softmax maps with a learned weight, a mixer to set
+ * beside full attention, with its gradient.  A row of Q and K holds two halves of d = head_dim / 2
+ * channels, a row of V and O all head_dim of them.  Per batch entry and head h, with
+ * Q = [Q1 | Q2], K = [K1 | K2]:
+ *     Pm = softmax(scale Qm Km^T) over the keys that a query sees,   O = P1 V - lambda_h P2 V,
+ *     lambda_h = exp(q1_h . k1_h) - exp(q2_h . k2_h) + init.
+ * Queries and keys have their own number here, and Q, K, V, O no grid: tokens are what n_q and
+ * n_k count (grid tokens and prefix tokens alike).
+ *  - Heads h * G .. h * G + G - 1, G = heads / kv_heads, share K and V head h (K, V, dK and dV have kv_heads heads).
+ *  - q_lengths, k_lengths: device arrays of `batch` numbers, or NULL (n_q, n_k): of sequence b only the
+ *    first q_lengths[b] queries and k_lengths[b] keys exist.  What lies behind them is not read; rows of O and
+ *    dQ behind a sequence's queries, and of dK and dV behind its keys, are written as zeros.
+ *    Numbers below 0 count as 0, above n_q or n_k as n_q or n_k.
+ *  - causal != 0: query i sees keys 0 .. i + k_lengths[b] - q_lengths[b] (the last query sees all keys).
+ *  - A query that sees no key has a zero row in O and in dQ.
+ * head_dim is 64 or 128 for both element types, o_dtype as in jv_attn_desc; at most 2^24 queries and keys and 65535
+ * batch entries times heads.  Strides as in jv_attn_desc; K and V may be broadcast (stride 0), rows of O may
+ * not overlap each other.  The stride of an axis of one is ignored.  scale <= 0 or NaN selects 1/sqrt(d).
+ * Arithmetic: JV_F32 on fp32 matrix instructions.  JV_BF16: the weights Pm are rounded to bf16 in front of the
+ * product with V, and in the gradient P1 - lambda P2 and the gradients of the logits in front of theirs; everything else is fp32.
+ * Device memory of a call, 256-byte aligned, sized by the queries below (0 for an invalid descriptor):
+ *   workspace  scratch of the call, contents unspecified afterwards; the forward pass may be given NULL
+ *              where its query says 256 (nothing is kept there then).
+ *   saved      forward: NULL, or memory that receives what the backward pass needs (the denominators of both
+ *              softmaxes, and P2 V in the element type).  o_dtype must be dtype then (JV_ERR_UNSUPPORTED).
+ * Outputs, `saved` and workspaces may not overlap each other or anything read.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    int32_t batch, heads, kv_heads; /* kv_heads divides heads */
+    int32_t n_q, n_k;               /* queries and keys of a sequence */
+    int32_t head_dim;               /* 64 or 128: channels of a row, both halves */
+    jv_dtype dtype;                 /* element type of Q, K, V */
+    jv_dtype o_dtype;               /* element type of O: equal to dtype, or JV_F32 with JV_BF16 inputs */
+    jv_strides q, k, v, o;
+    int32_t causal;
+    const int32_t *q_lengths, *k_lengths; /* device, or NULL */
+} jv_diff_attn_desc;
+
+/* lambda's parameters: device fp32 vectors of d numbers, one set for all heads (per_head = 0) or [heads, d]. */
+typedef struct {
+    const float *q1, *k1, *q2, *k2;
+    float init;
+    int32_t per_head;
+} jv_diff_lambda;
+
+size_t jv_diff_attn_workspace_bytes(const jv_diff_attn_desc *desc);
+size_t jv_diff_attn_saved_bytes(const jv_diff_attn_desc *desc);
+jv_status jv_diff_attn_fwd(const jv_diff_attn_desc *desc, const void *q, const void *k, const void *v,
+                           const jv_diff_lambda *lambda, void *o, float scale, void *saved,
+                           size_t saved_bytes, void *workspace, size_t workspace_bytes,
+                           void *hip_stream);
+
+/* Gradient of jv_diff_attn_fwd: desc, q, k, v, lambda and scale as in the forward call that filled `saved`, o its output, d_o the
+ * gradient of o.  All of desc's element type (o_dtype = dtype, JV_ERR_UNSUPPORTED otherwise).  With
+ * dP = dO V^T and Dm the row sums of dO o (Pm V):
+ *     dV = (P1 - lambda P2)^T dO,   dS1 = P1 o (dP - D1),   dS2 = -lambda P2 o (dP - D2),
+ *     dQm = scale dSm Km,   dKm = scale dSm^T Qm,   dlambda_h = - sum P2 o dP,
+ * dK and dV summed over the heads that share them.  d_q1 .. d_k2 receive the gradients of lambda's vectors in fp32, in their
+ * layout (summed over the heads where these share one set); all four, or none (NULL).
+ * The weights are formed again from the logarithm of their denominators, in fp32: off by 2^-24 of the logit's size, so that
+ * logits beyond 2^20 leave no gradient of use (the forward pass takes any that are finite).
+ * Sums have a fixed order (no atomics): the same call gives the same bits.  Rows of d_q, d_k, d_v may not overlap; d_q, d_k, d_v may be views of
+ * one buffer that lie between each other's rows. */
+typedef struct {
+    const void *d_o;      /* device, [batch, heads, n_q, head_dim] */
+    void *d_q, *d_k, *d_v;
+    jv_strides d_o_strides, d_q_strides, d_k_strides, d_v_strides;
+    float *d_q1, *d_k1, *d_q2, *d_k2; /* device, or all NULL */
+} jv_diff_attn_grads;
+
+size_t jv_diff_attn_bwd_workspace_bytes(const jv_diff_attn_desc *desc);
+jv_status jv_diff_attn_bwd(const jv_diff_attn_desc *desc, const void *q, const void *k, const void *v,
+                           const jv_diff_lambda *lambda, const void *o, const void *saved,
+                           size_t saved_bytes, const jv_diff_attn_grads *grads, float scale,
+                           void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* ---------------------------------------------------------------------------
  * Encoder pieces.  The paper's hybrid encoder keeps the pretrained block around each token
  * mixer (Sec. 3.2.3: the MLP and the attention projections W_Q, W_K, W_V, W_O are inherited
  * unchanged); the block is the standard pre-LN transformer block.
@@ -291,6 +368,22 @@ jv_status jv_layernorm_fwd(const void *x, const float *gamma, const float *beta,
 jv_status jv_gemm_bias_act(const void *a, const void *w, const float *bias, const void *residual,
                            void *y, int64_t M, int32_t N, int32_t K, jv_epilogue epilogue,
                            jv_dtype y_dtype, void *hip_stream);
+
+/* Gradient of jv_layernorm_fwd.  With xh = (x - mean) / sqrt(var + eps) and g = dy o gamma, per row of `cols`,
+ *     dx = (g - mean(g) - xh mean(g o xh)) / sqrt(var + eps)  (+ residual),
+ *     dgamma = sum over rows of dy o xh,   dbeta = sum over rows of dy,
+ * in fp32 throughout (mean and variance are formed again from x, in two passes over registers).  x is [rows, cols] of
+ * x_dtype, dy of dy_dtype, dx of x_dtype; residual, of x_dtype and x's shape, or NULL: a gradient that is added to
+ * dx before it is rounded, as that of the residual stream around a pre-LN branch (it may be dx itself; dx may not
+ * overlap anything else).  gamma, dgamma and dbeta are fp32 [cols]; dgamma and dbeta are overwritten, and may both
+ * be NULL (not formed).  rows contiguous, cols a multiple of 8 up to 8192, all pointers device, 16-byte aligned.
+ * workspace: jv_layernorm_bwd_workspace_bytes(rows, cols) bytes (0 for sizes that are refused), 256-byte
+ * aligned; it holds partial column sums, whose order depends on the sizes alone: the same call gives the same bits. */
+size_t jv_layernorm_bwd_workspace_bytes(int64_t rows, int32_t cols);
+jv_status jv_layernorm_bwd(const void *x, const float *gamma, const void *dy, const void *residual, void *dx,
+                           float *dgamma, float *dbeta, int64_t rows, int32_t cols, float eps,
+                           jv_dtype x_dtype, jv_dtype dy_dtype, void *workspace,
+                           size_t workspace_bytes, void *hip_stream);
 
 /* ---------------------------------------------------------------------------
  * Hybrid encoder forward (Fig. 2 of the paper: per layer, one of the three token mixers;

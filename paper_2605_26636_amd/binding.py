@@ -25,7 +25,9 @@ EXPORTS = [
     "jv_linear_block_workspace_bytes", "jv_linear_block_fwd", "jv_linear_block_focused_fwd",
     "jv_window_geometry", "jv_window_maps_host", "jv_window_maps_device",
     "jv_window_attn_fwd", "jv_full_attn_fwd",
-    "jv_layernorm_fwd", "jv_gemm_bias_act",
+    "jv_diff_attn_workspace_bytes", "jv_diff_attn_saved_bytes", "jv_diff_attn_fwd",
+    "jv_diff_attn_bwd_workspace_bytes", "jv_diff_attn_bwd",
+    "jv_layernorm_fwd", "jv_layernorm_bwd_workspace_bytes", "jv_layernorm_bwd", "jv_gemm_bias_act",
     "jv_encoder_create", "jv_encoder_workspace_bytes", "jv_encoder_forward", "jv_encoder_forward_taps", "jv_encoder_destroy",
     "jv_encoder_fold_bytes", "jv_encoder_fold_layernorm", "jv_encoder_fuse_linear_projection",
 ]
@@ -44,6 +46,25 @@ class JvAttnDesc(ctypes.Structure):
                 ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int), ("o_dtype", ctypes.c_int),
                 ("q", JvStrides), ("k", JvStrides), ("v", JvStrides), ("o", JvStrides),
                 ("n_prefix", ctypes.c_int32)]
+
+
+class JvDiffAttnDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("n_q", ctypes.c_int32), ("n_k", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int), ("o_dtype", ctypes.c_int),
+                ("q", JvStrides), ("k", JvStrides), ("v", JvStrides), ("o", JvStrides),
+                ("causal", ctypes.c_int32), ("q_lengths", ctypes.c_void_p), ("k_lengths", ctypes.c_void_p)]
+
+
+class JvDiffLambda(ctypes.Structure):
+    _fields_ = [("q1", ctypes.c_void_p), ("k1", ctypes.c_void_p), ("q2", ctypes.c_void_p), ("k2", ctypes.c_void_p),
+                ("init", ctypes.c_float), ("per_head", ctypes.c_int32)]
+
+
+class JvDiffAttnGrads(ctypes.Structure):
+    _fields_ = [("d_o", ctypes.c_void_p), ("d_q", ctypes.c_void_p), ("d_k", ctypes.c_void_p), ("d_v", ctypes.c_void_p),
+                ("d_o_strides", JvStrides), ("d_q_strides", JvStrides), ("d_k_strides", JvStrides), ("d_v_strides", JvStrides),
+                ("d_q1", ctypes.c_void_p), ("d_k1", ctypes.c_void_p), ("d_q2", ctypes.c_void_p), ("d_k2", ctypes.c_void_p)]
 
 
 class JvDwcParams(ctypes.Structure):
@@ -128,6 +149,18 @@ def lib():
                                        ctypes.c_int, vp]
         L.jv_gemm_bias_act.argtypes = [vp, vp, vp, vp, vp, i64, i32, i32, ctypes.c_int,
                                        ctypes.c_int, vp]
+        diff = ctypes.POINTER(JvDiffAttnDesc)
+        for name in ("jv_diff_attn_workspace_bytes", "jv_diff_attn_saved_bytes", "jv_diff_attn_bwd_workspace_bytes"):
+            getattr(L, name).restype = ctypes.c_size_t
+            getattr(L, name).argtypes = [diff]
+        L.jv_diff_attn_fwd.argtypes = [diff, vp, vp, vp, ctypes.POINTER(JvDiffLambda), vp, ctypes.c_float, vp,
+                                       ctypes.c_size_t, vp, ctypes.c_size_t, vp]
+        L.jv_diff_attn_bwd.argtypes = [diff, vp, vp, vp, ctypes.POINTER(JvDiffLambda), vp, vp, ctypes.c_size_t,
+                                       ctypes.POINTER(JvDiffAttnGrads), ctypes.c_float, vp, ctypes.c_size_t, vp]
+        L.jv_layernorm_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.jv_layernorm_bwd_workspace_bytes.argtypes = [i64, i32]
+        L.jv_layernorm_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i32, ctypes.c_float, ctypes.c_int, ctypes.c_int,
+                                       vp, ctypes.c_size_t, vp]
         L.jv_encoder_create.argtypes = [ctypes.POINTER(JvEncoderConfig),
                                         ctypes.POINTER(JvBlockWeights), ctypes.POINTER(vp)]
         L.jv_encoder_workspace_bytes.restype = ctypes.c_size_t
@@ -299,6 +332,103 @@ def jv_full_attn_fwd(q, k, v, o, grid, scale=0.0, stream=None):
     _check(st)
 
 
+def make_diff_desc(q, k, v, o, causal=False, q_lengths=None, k_lengths=None):
+    """Descriptor of differential attention for views q, o [B, heads, n_q, d] and k, v [B, kv_heads, n_k, d]; lengths are
+    int32 tensors [B] on the GPU."""
+    B, heads, n_q, d = q.shape
+    _, kv_heads, n_k, _ = k.shape
+    if tuple(o.shape) != tuple(q.shape) or tuple(v.shape) != tuple(k.shape) or tuple(k.shape) != (B, kv_heads, n_k, d):
+        raise ValueError("q and o must share one shape, and k and v one of the same batch and head_dim")
+    if not (q.dtype == k.dtype == v.dtype):
+        raise TypeError("q, k, v must share one dtype")
+    _same_device(q, k, v, o, q_lengths, k_lengths)
+    for t in (q_lengths, k_lengths):
+        if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (B,) or not t.is_contiguous()):
+            raise ValueError("lengths must be contiguous int32 tensors [B]")
+    return JvDiffAttnDesc(B, heads, kv_heads, n_q, n_k, d, _dtype_code(q), _dtype_code(o), _strides(q), _strides(k), _strides(v), _strides(o),
+                          1 if causal else 0, _ptr(q_lengths), _ptr(k_lengths))
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _same_device(first, *others):
+    for t in (first,) + others:
+        if t is not None and (not t.is_cuda or t.device != first.device):
+            raise ValueError("tensors must live on one GPU")
+
+
+def _diff_lambda(lam, init, q):
+    """jv_diff_lambda of four fp32 tensors (lambda_q1, lambda_k1, lambda_q2, lambda_k2), each [d] or [heads, d], d = head_dim / 2."""
+    shapes = ((q.shape[3] // 2,), (q.shape[1], q.shape[3] // 2))
+    shape = tuple(lam[0].shape)
+    if len(lam) != 4 or shape not in shapes:
+        raise ValueError("lambda has four vectors, each [head_dim / 2] or [heads, head_dim / 2]")
+    _check_vectors(lam, shape, q)
+    return JvDiffLambda(*[t.data_ptr() for t in lam], init, 1 if len(shape) == 2 else 0)
+
+
+def _check_vectors(vectors, shape, q):
+    _same_device(q, *vectors)
+    for t in vectors:
+        if t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape) != shape:
+            raise ValueError("lambda's vectors and their gradients must be contiguous fp32 tensors of one shape")
+
+
+def jv_diff_attn_workspace_bytes(desc):
+    return int(lib().jv_diff_attn_workspace_bytes(ctypes.byref(desc)))
+
+
+def jv_diff_attn_saved_bytes(desc):
+    return int(lib().jv_diff_attn_saved_bytes(ctypes.byref(desc)))
+
+
+def jv_diff_attn_bwd_workspace_bytes(desc):
+    return int(lib().jv_diff_attn_bwd_workspace_bytes(ctypes.byref(desc)))
+
+
+def _sized(t):
+    return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
+
+
+def jv_diff_attn_fwd(q, k, v, lam, o, lambda_init=0.8, scale=0.0, causal=False, q_lengths=None, k_lengths=None, saved=None,
+                     workspace=None, stream=None):
+    """o <- differential attention of (q, k, v); lam: four fp32 tensors [d] or [heads, d], d = head_dim / 2.  saved: a tensor of
+    jv_diff_attn_saved_bytes bytes that receives what the gradient needs.  Returns the workspace tensor used."""
+    desc = make_diff_desc(q, k, v, o, causal, q_lengths, k_lengths)
+    if workspace is None:
+        workspace = torch.empty(max(jv_diff_attn_workspace_bytes(desc), 256), dtype=torch.uint8, device=q.device)
+    _same_device(q, saved, workspace)
+    _check(lib().jv_diff_attn_fwd(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                  ctypes.byref(_diff_lambda(lam, lambda_init, q)), o.data_ptr(), scale, *_sized(saved),
+                                  *_sized(workspace), _stream(stream)))
+    return workspace
+
+
+def jv_diff_attn_bwd(q, k, v, lam, o, saved, d_o, d_q, d_k, d_v, d_lam=None, lambda_init=0.8, scale=0.0, causal=False,
+                     q_lengths=None, k_lengths=None, workspace=None, stream=None):
+    """d_q, d_k, d_v and d_lam (four tensors like lam, or None) <- the gradient of jv_diff_attn_fwd, whose other arguments
+    are given as they were there; returns the workspace tensor used."""
+    desc = make_diff_desc(q, k, v, o, causal, q_lengths, k_lengths)
+    for like, t in ((q, d_o), (q, d_q), (k, d_k), (v, d_v)):
+        if tuple(t.shape) != tuple(like.shape) or t.dtype != q.dtype:
+            raise ValueError("gradients must have the shape and dtype of their tensors")
+    _same_device(q, saved, d_o, d_q, d_k, d_v, workspace)
+    lam_arg = _diff_lambda(lam, lambda_init, q)
+    if d_lam is not None:
+        if len(d_lam) != 4:
+            raise ValueError("lambda has four vectors")
+        _check_vectors(d_lam, tuple(lam[0].shape), q)
+    if workspace is None:
+        workspace = torch.empty(max(jv_diff_attn_bwd_workspace_bytes(desc), 256), dtype=torch.uint8, device=q.device)
+    grads = JvDiffAttnGrads(d_o.data_ptr(), d_q.data_ptr(), d_k.data_ptr(), d_v.data_ptr(), _strides(d_o), _strides(d_q), _strides(d_k),
+                            _strides(d_v), *([t.data_ptr() for t in d_lam] if d_lam is not None else [None] * 4))
+    _check(lib().jv_diff_attn_bwd(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), ctypes.byref(lam_arg), o.data_ptr(),
+                                  *_sized(saved), ctypes.byref(grads), scale, *_sized(workspace), _stream(stream)))
+    return workspace
+
+
 def jv_window_geometry(grid_h, grid_w, win_h, win_w):
     """(padded_h, padded_w, n_windows); host computation."""
     out = (ctypes.c_int32 * 3)()
@@ -337,6 +467,31 @@ def jv_layernorm_fwd(x, gamma, beta, y, eps=1e-6, stream=None):
         raise ValueError("x and y must be contiguous [rows, cols]")
     _check(lib().jv_layernorm_fwd(x.data_ptr(), gamma.data_ptr(), beta.data_ptr(), y.data_ptr(),
                                   rows, cols, eps, _dtype_code(x), _dtype_code(y), _stream(stream)))
+
+
+def jv_layernorm_bwd_workspace_bytes(rows, cols):
+    return int(lib().jv_layernorm_bwd_workspace_bytes(rows, cols))
+
+
+def jv_layernorm_bwd(x, gamma, dy, dx, dgamma=None, dbeta=None, eps=1e-6, residual=None, workspace=None, stream=None):
+    """dx <- gradient of LayerNorm(x) over the last axis (+ residual), dgamma, dbeta <- those of its scale and shift (both, or
+    neither); x, dx and residual of one type, dy fp32 or bf16, all [rows, cols], gamma, dgamma, dbeta fp32 [cols].
+    Returns the workspace tensor used."""
+    rows, cols = x.shape
+    _same_device(x, gamma, dy, dx, dgamma, dbeta, residual, workspace)
+    for t in (x, dy, dx, residual):
+        if t is not None and not (t.is_contiguous() and tuple(t.shape) == (rows, cols)):
+            raise ValueError("x, dy, dx and residual must be contiguous [rows, cols]")
+    if dx.dtype != x.dtype or (residual is not None and residual.dtype != x.dtype):
+        raise TypeError("dx and residual must have x's dtype")
+    for t in (gamma, dgamma, dbeta):
+        if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape) != (cols,)):
+            raise ValueError("gamma, dgamma and dbeta must be contiguous fp32 [cols]")
+    if workspace is None:
+        workspace = torch.empty(max(jv_layernorm_bwd_workspace_bytes(rows, cols), 256), dtype=torch.uint8, device=x.device)
+    _check(lib().jv_layernorm_bwd(x.data_ptr(), gamma.data_ptr(), dy.data_ptr(), _ptr(residual), dx.data_ptr(), _ptr(dgamma), _ptr(dbeta),
+                                  rows, cols, eps, _dtype_code(x), _dtype_code(dy), *_sized(workspace), _stream(stream)))
+    return workspace
 
 
 def jv_gemm_bias_act(a, w, bias, residual, y, epilogue=JV_EPI_NONE, stream=None):

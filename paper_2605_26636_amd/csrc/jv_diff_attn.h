@@ -1,0 +1,226 @@
+// Differential attention (jv_diff_attn_fwd, jv_diff_attn_bwd): the problem as its kernels see it, and the tiles they share.
+//
+// Per (batch, head), with rows of W = head_dim channels, Q = [Q1 | Q2], K = [K1 | K2] in halves of W / 2:
+//     Pm = softmax(scale Qm Km^T) over the keys a row sees,  O = P1 V - lambda P2 V.
+// All products run as D = A B + C on 32 x 32 blocks whose columns are what a wavefront keeps (its queries, or its keys in
+// the key pass of the gradient) and whose rows are the tokens of the tile that passes through LDS; a lane holds one
+// column, so that softmax sums stay inside a lane (and the lane 32 further), and a finished block is the B
+// operand of the next product as it stands.  fp32 tensors take the same steps on fp32 matrix instructions.
+#pragma once
+
+#include <type_traits>
+
+#include "jv_common.h"
+#include "jv_mfma.h"
+
+namespace jv {
+
+struct DiffArgs {
+    TensorArg q, k, v, o;
+    int B, heads, kv_heads, group;  // group: heads that share one K and V
+    int n_q, n_k, causal;
+    const int *q_len, *k_len;       // [B], or null
+    float scale, c;                 // c = scale log2(e)
+    const float *lq1, *lk1, *lq2, *lk2;
+    float l_init;
+    int l_step;                     // W / 2: a set of vectors for every head; 0: one set
+    float *lse;                     // saved: [2][B * heads * n_q], log2 of the softmax denominators; or null
+    void *o2;                       // saved: [B * heads * n_q][W], P2 V
+    // forward pass over parts of the keys
+    float *part;
+    int splits, tiles_per_split;
+    // gradient
+    TensorArg d_o, dq, dk, dv;
+    float *rows_d;                  // [2][B * heads * n_q]: rowsum(dO o Om)
+    float *lam_part;                // [B * heads * row blocks]: sums of P2 o dP
+    float *dlq1, *dlk1, *dlq2, *dlk2;
+    int blocks;                     // blocks of rows (or keys) a (batch, head) has
+    long long items;                // workgroups with work
+};
+
+struct DiffProblem {
+    DiffArgs a;
+    int W;
+    bool bf16, o_bf16;
+};
+
+// Workgroup -> item: contiguous ranges per XCD (workgroup w runs on XCD w % 8), so that the workgroups of a (batch, head)
+// share its K and V in one L2.
+__device__ inline long long diff_item(long long items) {
+    const long long per = (items + 7) / 8;
+    return (long long)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+}
+inline unsigned diff_grid(long long items) { return (unsigned)(8 * ((items + 7) / 8)); }
+
+constexpr int kDiffTile = 32;  // tokens of a tile
+
+// Tokens [0, limit) of a sequence that query qi sees, by the lengths of the sequence.
+struct DiffLengths {
+    int q, k;
+    __device__ DiffLengths(const DiffArgs &a, int b) {
+        q = a.q_len ? min(max(a.q_len[b], 0), a.n_q) : a.n_q;
+        k = a.k_len ? min(max(a.k_len[b], 0), a.n_k) : a.n_k;
+    }
+    __device__ int limit(const DiffArgs &a, int qi) const {
+        if (qi >= q) return 0;
+        return a.causal ? min(max(qi + 1 + k - q, 0), k) : k;
+    }
+};
+
+// Eight channels of one token, or eight tokens of one channel: an operand of a product over 16 of them (lane = 32 g + i
+// holds row or column i and elements 8 g .. + 7, or what the other operand holds there).
+template <typename T> struct DiffFrag;
+template <> struct DiffFrag<__bf16> { bf16x8 x; };
+template <> struct DiffFrag<float> { f32x4 x[2]; };
+
+__device__ inline f32x16 diff_mma(const DiffFrag<__bf16> &a, const DiffFrag<__bf16> &b, f32x16 c) { return mfma32(a.x, b.x, c); }
+__device__ inline f32x16 diff_mma(const DiffFrag<float> &a, const DiffFrag<float> &b, f32x16 c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[e >> 2][e & 3], b.x[e >> 2][e & 3], c, 0, 0, 0);
+    return c;
+}
+__device__ inline void diff_zero(f32x16 &x) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) x[v] = 0.f;
+}
+// Rows 16 kk .. + 15 of a finished block as B operand: element e of lane 32 g + i is row 16 kk + 8 (e / 4) + 4 g + e % 4.
+template <typename T>
+__device__ inline DiffFrag<T> diff_block_frag(const f32x16 &s, int kk) {
+    DiffFrag<T> f;
+    if constexpr (std::is_same_v<T, __bf16>) {
+        f.x = as_bf16x8(u32x4{pack_bf16x2(s[8 * kk], s[8 * kk + 1]), pack_bf16x2(s[8 * kk + 2], s[8 * kk + 3]),
+                              pack_bf16x2(s[8 * kk + 4], s[8 * kk + 5]), pack_bf16x2(s[8 * kk + 6], s[8 * kk + 7])});
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f.x[e >> 2][e & 3] = s[8 * kk + e];
+    }
+    return f;
+}
+// Channels 16 ks + 8 g .. + 7 of a row in memory.
+template <typename T>
+__device__ inline DiffFrag<T> diff_global_frag(const T *row, int ks, int g, bool live) {
+    DiffFrag<T> f;
+    if constexpr (std::is_same_v<T, __bf16>) {
+        f.x = as_bf16x8(live ? *(const u32x4 *)(row + 16 * ks + 8 * g) : u32x4{0, 0, 0, 0});
+    } else {
+#pragma unroll
+        for (int p = 0; p < 2; ++p) f.x[p] = live ? *(const f32x4 *)(row + 16 * ks + 8 * g + 4 * p) : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    return f;
+}
+
+// 32 rows of W channels in LDS.  16-byte chunks are moved inside their row so that both kinds of reads spread over
+// all banks: a chunk of 16 consecutive rows (row-per-lane operands), and, for 16-bit elements, 64 bytes of four
+// consecutive rows (transposing reads), for 32-bit ones 128 bytes of two rows four apart (channel-per-lane reads).
+template <typename T, int W>
+struct DiffTile {
+    static constexpr int kRowBytes = W * (int)sizeof(T), kChunks = kRowBytes / 16, kBytes = kDiffTile * kRowBytes;
+    __device__ static unsigned off(int row, int chunk) {
+        unsigned slot;
+        if constexpr (sizeof(T) == 4) slot = chunk ^ ((row & 3) | (row & 4) << 1 | (row & 8) >> 1);
+        else if constexpr (W == 128) slot = chunk ^ ((row & 3) << 2 | (row >> 2 & 3));
+        else slot = chunk ^ ((row >> 1 & 1) << 2 | (row >> 2 & 3));
+        return row * kRowBytes + slot * 16;
+    }
+    // Channels 16 ks + 8 g .. + 7 of row `row`.
+    __device__ static DiffFrag<T> row_frag(const unsigned char *tile, int row, int ks, int g) {
+        DiffFrag<T> f;
+        if constexpr (sizeof(T) == 2) {
+            f.x = as_bf16x8(*(const u32x4 *)(tile + off(row, 2 * ks + g)));
+        } else {
+            f.x[0] = *(const f32x4 *)(tile + off(row, 4 * ks + 2 * g));
+            f.x[1] = *(const f32x4 *)(tile + off(row, 4 * ks + 2 * g + 1));
+        }
+        return f;
+    }
+    // Channel 32 cb + i, rows as diff_block_frag has them.
+    __device__ static DiffFrag<T> col_frag(const unsigned char *tile, int kk, int cb, int lane) {
+        DiffFrag<T> f;
+        const int g = lane >> 5;
+        if constexpr (sizeof(T) == 2) {
+            const int b = lane >> 4, j = lane & 15, chunk = cb * 4 + (b & 1) * 2 + ((j & 3) >> 1), row = 16 * kk + 4 * g + (j >> 2);
+            const u32x2 r0 = lds_read_tr16(tile + off(row, chunk) + (j & 1) * 8), r1 = lds_read_tr16(tile + off(row + 8, chunk) + (j & 1) * 8);
+            f.x = as_bf16x8(u32x4{r0[0], r0[1], r1[0], r1[1]});
+        } else {
+            const int ch = 32 * cb + (lane & 31);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                f.x[e >> 2][e & 3] = *(const float *)(tile + off(16 * kk + 8 * (e >> 2) + 4 * g + (e & 3), ch >> 2) + (ch & 3) * 4);
+        }
+        return f;
+    }
+};
+
+// A tile on its way from memory into LDS through the registers of THREADS threads: fetched while the tile before it is
+// worked on.  Rows at `limit` and beyond are not read and arrive as zeros.
+template <typename T, int W, int THREADS>
+struct DiffFetch {
+    using Tile = DiffTile<T, W>;
+    static constexpr int kPieces = kDiffTile * Tile::kChunks / THREADS;
+    static_assert(kPieces * THREADS == kDiffTile * Tile::kChunks, "whole pieces a thread");
+    u32x4 x[kPieces];
+    __device__ void fetch(const T *base, long long sn, int row0, int limit, int tid) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int p = tid + THREADS * i, row = row0 + p / Tile::kChunks;
+            x[i] = row < limit ? *(const u32x4 *)((const char *)(base + (long long)row * sn) + (p % Tile::kChunks) * 16) : u32x4{0, 0, 0, 0};
+        }
+    }
+    __device__ void store(unsigned char *tile, int tid) const {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int p = tid + THREADS * i;
+            *(u32x4 *)(tile + Tile::off(p / Tile::kChunks, p % Tile::kChunks)) = x[i];
+        }
+    }
+};
+
+// lambda of head h: exp(lq1 . lk1) - exp(lq2 . lk2) + init, and its two exponentials, in every lane of the wavefront.
+struct DiffLambda {
+    float e1, e2, value;
+};
+template <int W>
+__device__ inline DiffLambda diff_lambda(const DiffArgs &a, int h, int lane) {
+    const int at = h * a.l_step + lane;
+    float x1 = 0.f, x2 = 0.f;
+    if (lane < W / 2) {
+        x1 = a.lq1[at] * a.lk1[at];
+        x2 = a.lq2[at] * a.lk2[at];
+    }
+    DiffLambda l;
+    l.e1 = expf(wave_sum(x1));
+    l.e2 = expf(wave_sum(x2));
+    l.value = l.e1 - l.e2 + a.l_init;
+    return l;
+}
+
+// Four consecutive channels of an output row.
+__device__ inline void diff_store4(float *p, f32x4 x) { *(f32x4 *)p = x; }
+__device__ inline void diff_store4(__bf16 *p, f32x4 x) { *(u32x2 *)p = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])}; }
+
+// Query rows of all sequences and heads.
+__host__ __device__ inline long long diff_rows(const DiffArgs &a) { return (long long)a.B * a.heads * a.n_q; }
+
+// Validates the descriptor, and with it the base pointers of q, k, v, o.
+jv_status diff_problem(const jv_diff_attn_desc *desc, const void *q, const void *k, const void *v, void *o,
+                       const jv_diff_lambda *lambda, float scale, DiffProblem *out);
+jv_status diff_check_desc(const jv_diff_attn_desc *desc);
+// Strides of a [b, h, n, W] tensor; a written one must have a place of its own for every row.
+jv_status diff_check_strides(const char *name, const jv_strides &s, int64_t b, int64_t h, int64_t n, int W, int64_t align, bool written);
+int64_t diff_span(const jv_strides &s, int64_t b, int64_t h, int64_t n, int W);  // elements up to the end of the last row
+size_t diff_saved_bytes(const jv_diff_attn_desc *desc);
+void diff_use_saved(DiffProblem *p, void *saved);
+
+// Kernels are built for two types and two widths: f(DiffKind of the call).
+template <typename ELEM, int WIDTH>
+struct DiffKind {
+    using T = ELEM;
+    static constexpr int W = WIDTH;
+};
+template <typename F>
+jv_status diff_with_kind(bool bf16, int W, F f) {
+    if (bf16) return W == 128 ? f(DiffKind<__bf16, 128>()) : f(DiffKind<__bf16, 64>());
+    return W == 128 ? f(DiffKind<float, 128>()) : f(DiffKind<float, 64>());
+}
+
+}  // namespace jv

@@ -1,0 +1,494 @@
+// Forward pass of differential attention, and what its entry points check on the host.
+//
+// A wavefront keeps 32 rows (queries) as columns and walks the keys in tiles of 32: scores of both maps, S^T = K Q^T with half
+// the channels each, two running softmaxes, and O1^T, O2^T += V^T P with every V operand read once for both maps.
+// The difference is formed at the end, in fp32.  24 matrix instructions of 32 x 32 x 16 a tile and wavefront (W = 128),
+// against 32 exponentials a lane.
+#include <math.h>
+#include <stdlib.h>
+
+#include <algorithm>
+
+#include "jv_diff_attn.h"
+
+namespace jv {
+
+constexpr float kDiffLazySum = 256.0f;  // largest lane sum of a tile taken without a search for its maximum
+
+// Running softmax of one map: reference m (log2 units; -inf before the first key seen), what a tile's weights are first tried
+// with (-m, or +inf), this lane's half of the sum, and the unnormalised output, channels 32 cb + 8 (v / 4) + 4 g + v % 4 of the lane's row.
+template <int W>
+struct DiffMap {
+    float m, minus_m, l;
+    f32x16 acc[W / 32];
+};
+
+__device__ inline float diff_exp(f32x16 &p, const f32x16 &s, float c, float minus_m) {
+    float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; v += 2) {
+        p[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, minus_m));
+        p[v + 1] = __builtin_amdgcn_exp2f(fmaf(s[v + 1], c, minus_m));
+        sum0 += p[v];
+        sum1 += p[v + 1];
+    }
+    return sum0 + sum1;
+}
+// Raises the reference to the tile's maximum and forms the weights against it from rounded products, whose maximum the
+// reference is (from exact ones a weight could be 2^(|m| 2^-24)).
+template <int W>
+__device__ inline float diff_raise(DiffMap<W> &w, f32x16 &p, const f32x16 &s, float c) {
+#pragma clang fp contract(off)
+    float t = s[0];
+#pragma unroll
+    for (int v = 1; v < 16; ++v) t = fmaxf(t, s[v]);
+    float lo, hi;
+    pair_values(t * c, &lo, &hi);  // this lane and lane ^ 32 share the row
+    const float m_new = fmaxf(w.m, fmaxf(lo, hi));
+    const float alpha = w.m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(w.m - m_new);
+    w.m = m_new;
+    w.l *= alpha;
+#pragma unroll
+    for (int cb = 0; cb < W / 32; ++cb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) w.acc[cb][v] *= alpha;
+    w.minus_m = fabsf(m_new) < 16777216.f ? -m_new : INFINITY;  // (so large that products must be rounded first: no tile is tried; NaN too)
+    const float ref = m_new == -INFINITY ? 0.f : m_new;
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        p[v] = __builtin_amdgcn_exp2f(s[v] * c - ref);
+        sum += p[v];
+    }
+    return sum;
+}
+// Weights of a tile against the present reference, which is raised only where they come out large (numerator and denominator always
+// use the same one).  Without a reference minus_m is +inf, so every tile raises until a key is seen; where all is masked (s = -inf)
+// the reference stays -inf and the weights, taken against 0, are zero.
+template <int W>
+__device__ inline void diff_softmax(DiffMap<W> &w, f32x16 &p, const f32x16 &s, float c) {
+    float sum = diff_exp(p, s, c, w.minus_m);
+    if (__builtin_amdgcn_ballot_w64(!(sum <= kDiffLazySum)) != 0) sum = diff_raise<W>(w, p, s, c);
+    w.l += sum;
+}
+
+// Rows of a (batch, kv head) are its group's heads one after the other, n_q queries each, so that a few queries of heads
+// that share K and V share a tile too.  WAVES x 32 rows a workgroup.
+// SPLIT: a workgroup takes a part of the keys and leaves (m, l) of both maps and the unnormalised outputs in a.part.
+template <typename T, typename TO, int W, int WAVES, bool SPLIT>
+__global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 2 : 1) diff_attn_fwd_kernel(DiffArgs a) {
+    using Tile = DiffTile<T, W>;
+    constexpr int THREADS = 64 * WAVES, KS = W / 16, CB = W / 32;
+    __shared__ __align__(16) unsigned char smem[2][2][Tile::kBytes];
+    __shared__ int wave_most[WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = tid >> 6;
+    long long item = diff_item(a.items);
+    if (item >= a.items) return;  // whole workgroup
+    const int split = SPLIT ? (int)(item % a.splits) : 0;
+    if (SPLIT) item /= a.splits;
+    const int block = a.blocks - 1 - (int)(item % a.blocks);  // causal: the longest rows first
+    const int bkv = (int)(item / a.blocks), b = bkv / a.kv_heads, kv = bkv % a.kv_heads;
+    const DiffLengths len(a, b);
+
+    const int n_rows = a.group * a.n_q, r = (block * WAVES + wave) * 32 + li;
+    const bool row_live = r < n_rows;
+    const int hg = row_live ? r / a.n_q : 0, qi = row_live ? r - hg * a.n_q : 0, head = kv * a.group + hg;
+    const int limit = row_live ? len.limit(a, qi) : 0;
+    int most = limit, least = row_live ? limit : a.n_k;
+#pragma unroll
+    for (int x = 1; x < 32; x *= 2) {
+        most = max(most, __shfl_xor(most, x));
+        least = min(least, __shfl_xor(least, x));
+    }
+    int wg_most = most;
+    if (WAVES > 1) {
+        if (lane == 0) wave_most[wave] = most;
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < WAVES; ++x) wg_most = max(wg_most, wave_most[x]);
+    }
+    int tile = SPLIT ? split * a.tiles_per_split : 0, tile_end = (wg_most + kDiffTile - 1) / kDiffTile;
+    if (SPLIT) tile_end = min(tile_end, tile + a.tiles_per_split);
+
+    DiffFrag<T> q[KS];
+    {
+        const T *row = (const T *)a.q.ptr + b * a.q.sb + head * a.q.sh + qi * a.q.sn;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) q[ks] = diff_global_frag<T>(row, ks, g, limit > 0);
+    }
+    DiffMap<W> w1, w2;
+    w1.m = w2.m = -INFINITY;
+    w1.minus_m = w2.minus_m = INFINITY;
+    w1.l = w2.l = 0.f;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+        diff_zero(w1.acc[cb]);
+        diff_zero(w2.acc[cb]);
+    }
+
+    const T *kbase = (const T *)a.k.ptr + b * a.k.sb + kv * a.k.sh, *vbase = (const T *)a.v.ptr + b * a.v.sb + kv * a.v.sh;
+    DiffFetch<T, W, THREADS> kf, vf;
+    auto fetch = [&](int t) {
+        kf.fetch(kbase, a.k.sn, t * kDiffTile, len.k, tid);
+        vf.fetch(vbase, a.v.sn, t * kDiffTile, len.k, tid);
+    };
+    if (tile < tile_end) {
+        fetch(tile);
+        kf.store(smem[0][0], tid);
+        vf.store(smem[0][1], tid);
+    }
+    lds_barrier();
+    for (int at = 0; tile < tile_end; ++tile, at ^= 1) {
+        const bool more = tile + 1 < tile_end;
+        if (more) fetch(tile + 1);
+        if (tile * kDiffTile < most) {  // (uniform in the wavefront)
+            const unsigned char *kt = smem[at][0], *vt = smem[at][1];
+            f32x16 s1, s2;
+            diff_zero(s1);
+            diff_zero(s2);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const DiffFrag<T> k = Tile::row_frag(kt, li, ks, g);
+                if (ks < KS / 2) s1 = diff_mma(k, q[ks], s1);
+                else s2 = diff_mma(k, q[ks], s2);
+            }
+            if ((tile + 1) * kDiffTile > least) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const bool hidden = tile * kDiffTile + 8 * (v / 4) + 4 * g + v % 4 >= limit;
+                    s1[v] = hidden ? -INFINITY : s1[v];
+                    s2[v] = hidden ? -INFINITY : s2[v];
+                }
+            }
+            DiffFrag<T> p1[2], p2[2];
+            f32x16 p;
+            diff_softmax<W>(w1, p, s1, a.c);
+            p1[0] = diff_block_frag<T>(p, 0);
+            p1[1] = diff_block_frag<T>(p, 1);
+            diff_softmax<W>(w2, p, s2, a.c);
+            p2[0] = diff_block_frag<T>(p, 0);
+            p2[1] = diff_block_frag<T>(p, 1);
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) {
+                    const DiffFrag<T> v = Tile::col_frag(vt, kk, cb, lane);
+                    w1.acc[cb] = diff_mma(v, p1[kk], w1.acc[cb]);
+                    w2.acc[cb] = diff_mma(v, p2[kk], w2.acc[cb]);
+                }
+        }
+        if (more) {
+            kf.store(smem[at ^ 1][0], tid);
+            vf.store(smem[at ^ 1][1], tid);
+        }
+        lds_barrier();
+    }
+
+    float lo, hi;
+    pair_values(w1.l, &lo, &hi);
+    const float l1 = lo + hi;
+    pair_values(w2.l, &lo, &hi);
+    const float l2 = lo + hi;
+    if (SPLIT) {
+        if (!row_live) return;
+        float *part = a.part + ((long long)split * a.B * a.kv_heads * n_rows + (long long)bkv * n_rows + r) * (2 * W + 4);
+        if (g == 0) *(f32x4 *)part = f32x4{w1.m, l1, w2.m, l2};
+        if (w1.m == -INFINITY && w2.m == -INFINITY) return;  // no key of this part is seen: not read again either
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                const f32x16 &x = w1.acc[cb], &y = w2.acc[cb];
+                *(f32x4 *)(part + 4 + 32 * cb + 8 * q4 + 4 * g) = f32x4{x[4 * q4], x[4 * q4 + 1], x[4 * q4 + 2], x[4 * q4 + 3]};
+                *(f32x4 *)(part + 4 + W + 32 * cb + 8 * q4 + 4 * g) = f32x4{y[4 * q4], y[4 * q4 + 1], y[4 * q4 + 2], y[4 * q4 + 3]};
+            }
+        return;
+    }
+    float lam = 0.f;
+    for (int h = __builtin_amdgcn_readfirstlane(head), last = kv * a.group + min((block * WAVES + wave) * 32 + 31, n_rows - 1) / a.n_q; h <= last; ++h) {
+        const float x = diff_lambda<W>(a, h, lane).value;
+        if (head == h) lam = x;
+    }
+    if (!row_live) return;
+    const float inv1 = l1 > 0.f ? 1.f / l1 : l1, inv2 = l2 > 0.f ? 1.f / l2 : l2;  // (0 for a row that sees nothing, NaN stays NaN)
+    const long long row = ((long long)b * a.heads + head) * a.n_q + qi;
+    if (a.lse && g == 0) {
+        a.lse[row] = w1.m == -INFINITY ? INFINITY : w1.m + log2f(l1);
+        a.lse[diff_rows(a) + row] = w2.m == -INFINITY ? INFINITY : w2.m + log2f(l2);
+    }
+    TO *o = (TO *)const_cast<void *>(a.o.ptr) + b * a.o.sb + head * a.o.sh + qi * a.o.sn;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+            const int ch = 32 * cb + 8 * q4 + 4 * g;
+            f32x4 x, y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                y[e] = w2.acc[cb][4 * q4 + e] * inv2;
+                x[e] = fmaf(-lam, y[e], w1.acc[cb][4 * q4 + e] * inv1);
+            }
+            diff_store4(o + ch, x);
+            if (a.o2) diff_store4((T *)a.o2 + row * W + ch, y);
+        }
+}
+
+// The parts of a row joined, in their order: one wavefront a row.
+template <typename T, typename TO, int W>
+__global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
+    const int lane = threadIdx.x & 63, n_rows = a.group * a.n_q;
+    const long long all = (long long)a.B * a.kv_heads * n_rows, at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (at >= all) return;
+    const int bkv = (int)(at / n_rows), r = (int)(at % n_rows), b = bkv / a.kv_heads, kv = bkv % a.kv_heads;
+    const int hg = r / a.n_q, qi = r - hg * a.n_q, head = kv * a.group + hg;
+    f32x4 ml = {-INFINITY, 0.f, -INFINITY, 0.f};
+    if (lane < a.splits) ml = *(const f32x4 *)(a.part + ((long long)lane * all + at) * (2 * W + 4));
+    float m1 = ml[0], m2 = ml[2];
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) {
+        m1 = fmaxf(m1, __shfl_xor(m1, x));
+        m2 = fmaxf(m2, __shfl_xor(m2, x));
+    }
+    const float f1 = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m1), f2 = ml[2] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[2] - m2);
+    const float l1 = wave_sum(ml[1] * f1), l2 = wave_sum(ml[3] * f2);
+    const unsigned long long seen = __builtin_amdgcn_ballot_w64(ml[0] != -INFINITY || ml[2] != -INFINITY);
+    constexpr int PER = W / 64;
+    float x1[PER] = {}, x2[PER] = {};
+    for (int s = 0; s < a.splits; ++s) {
+        if (!(seen >> s & 1)) continue;
+        const float *part = a.part + ((long long)s * all + at) * (2 * W + 4) + 4 + lane * PER;
+        const float g1 = __shfl(f1, s), g2 = __shfl(f2, s);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            x1[e] = fmaf(part[e], g1, x1[e]);
+            x2[e] = fmaf(part[W + e], g2, x2[e]);
+        }
+    }
+    const float lam = diff_lambda<W>(a, head, lane).value;
+    const float inv1 = l1 > 0.f ? 1.f / l1 : l1, inv2 = l2 > 0.f ? 1.f / l2 : l2;
+    const long long row = ((long long)b * a.heads + head) * a.n_q + qi;
+    if (a.lse && lane == 0) {
+        a.lse[row] = m1 == -INFINITY ? INFINITY : m1 + log2f(l1);
+        a.lse[diff_rows(a) + row] = m2 == -INFINITY ? INFINITY : m2 + log2f(l2);
+    }
+    TO *o = (TO *)const_cast<void *>(a.o.ptr) + b * a.o.sb + head * a.o.sh + qi * a.o.sn + lane * PER;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        const float y = x2[e] * inv2;
+        o[e] = (TO)fmaf(-lam, y, x1[e] * inv1);
+        if (a.o2) ((T *)a.o2)[row * W + lane * PER + e] = (T)y;
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------------------
+
+// How a forward pass is cut: wavefronts a workgroup (32 rows each) and parts of the keys.  Up to 64 rows (a few queries, all heads
+// of a group together) take one wavefront each; more take workgroups of four, which share the tiles.  Keys are cut where
+// the launch would leave units idle: into as many parts as fill about two workgroups of four wavefronts a unit, of
+// four tiles at least, at most 64 (a wavefront of the join holds one part a lane).
+struct DiffPlan {
+    int waves, blocks, splits, tiles_per_split;
+};
+static DiffPlan diff_plan(int B, int kv_heads, long long n_rows, int n_k) {
+    DiffPlan p;
+    p.waves = n_rows <= 64 ? 1 : 4;
+    p.blocks = (int)((n_rows + 32 * p.waves - 1) / (32 * p.waves));
+    const long long groups = (long long)B * kv_heads * p.blocks, tiles = (n_k + kDiffTile - 1) / kDiffTile;
+    const long long want = p.waves == 1 ? 2048 : 512;
+    long long splits = groups * 2 > want ? 1 : want / groups;
+    splits = std::max(1ll, std::min({splits, tiles / 4, 64ll}));
+    p.tiles_per_split = (int)((tiles + splits - 1) / splits);
+    p.splits = (int)((tiles + p.tiles_per_split - 1) / p.tiles_per_split);
+    return p;
+}
+static size_t diff_part_bytes(const DiffPlan &p, long long rows, int W) {
+    return p.splits > 1 ? (size_t)p.splits * rows * (2 * W + 4) * 4 : 0;
+}
+
+jv_status diff_check_strides(const char *name, const jv_strides &s, int64_t b, int64_t h, int64_t n, int W, int64_t align, bool written) {
+    const int64_t size[3] = {b, h, n}, stride[3] = {s.stride_b, s.stride_h, s.stride_n};
+    int64_t reach = W;  // elements up to the end of the last row
+    for (int i = 0; i < 3; ++i) {
+        if (size[i] == 1) continue;  // the stride of an axis of one is not used
+        if (stride[i] < 0) return fail(JV_ERR_INVALID_ARG, "%s: negative stride", name);
+        if (i == 2 && stride[i] < W) return fail(JV_ERR_INVALID_ARG, "%s: stride_n < head_dim", name);
+        if (stride[i] % align) return fail(JV_ERR_INVALID_ARG, "%s: strides must keep rows 16-byte aligned", name);
+        if (stride[i] > (INT64_C(1) << 56) / size[i]) return fail(JV_ERR_INVALID_ARG, "%s: strides reach beyond the address space", name);
+        reach += (size[i] - 1) * stride[i];
+    }
+    if (reach > INT64_C(1) << 57) return fail(JV_ERR_INVALID_ARG, "%s: strides reach beyond the address space", name);
+    if (written) {  // every row a place of its own: each axis steps over all that the axes of smaller strides span
+        int order[3] = {0, 1, 2};
+        std::sort(order, order + 3, [&](int x, int y) { return stride[x] < stride[y]; });
+        int64_t span = W;
+        for (int i : order) {
+            if (size[i] == 1) continue;
+            if (stride[i] < span) return fail(JV_ERR_INVALID_ARG, "%s: rows of a tensor that is written overlap", name);
+            span += (size[i] - 1) * stride[i];
+        }
+    }
+    return JV_OK;
+}
+
+int64_t diff_span(const jv_strides &s, int64_t b, int64_t h, int64_t n, int W) {
+    return (b - 1) * s.stride_b + (h - 1) * s.stride_h + (n - 1) * s.stride_n + W;  // (an axis of one adds nothing)
+}
+
+jv_status diff_check_desc(const jv_diff_attn_desc *d) {
+    if (!d) return fail(JV_ERR_INVALID_ARG, "descriptor is null");
+    if (d->batch <= 0 || d->heads <= 0 || d->kv_heads <= 0 || d->n_q <= 0 || d->n_k <= 0)
+        return fail(JV_ERR_INVALID_ARG, "batch, heads, kv_heads, n_q, n_k must be positive");
+    if (d->heads % d->kv_heads) return fail(JV_ERR_INVALID_ARG, "heads must be a multiple of kv_heads");
+    if (d->n_q > (1 << 24) || d->n_k > (1 << 24)) return fail(JV_ERR_UNSUPPORTED, "more than 2^24 queries or keys");
+    if ((int64_t)d->batch * d->heads > 65535) return fail(JV_ERR_UNSUPPORTED, "batch * heads above 65535");
+    if ((int64_t)d->heads / d->kv_heads * d->n_q > (1 << 30)) return fail(JV_ERR_UNSUPPORTED, "more than 2^30 queries of a kv head");
+    if (d->head_dim <= 0) return fail(JV_ERR_INVALID_ARG, "head_dim must be positive");
+    if (d->head_dim != kHeadDim && d->head_dim != kHeadDimWide) return fail(JV_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+    if ((d->dtype != JV_F32 && d->dtype != JV_BF16) || (d->o_dtype != JV_F32 && d->o_dtype != JV_BF16))
+        return fail(JV_ERR_INVALID_ARG, "unknown dtype");
+    if (d->dtype == JV_F32 && d->o_dtype != JV_F32) return fail(JV_ERR_UNSUPPORTED, "fp32 inputs need an fp32 output");
+    if (((uintptr_t)d->q_lengths | (uintptr_t)d->k_lengths) & 3) return fail(JV_ERR_INVALID_ARG, "lengths must be 4-byte aligned");
+    const int64_t in = d->dtype == JV_BF16 ? 8 : 4, out = d->o_dtype == JV_BF16 ? 8 : 4;
+    jv_status st;
+    if ((st = diff_check_strides("q", d->q, d->batch, d->heads, d->n_q, d->head_dim, in, false)) != JV_OK) return st;
+    if ((st = diff_check_strides("k", d->k, d->batch, d->kv_heads, d->n_k, d->head_dim, in, false)) != JV_OK) return st;
+    if ((st = diff_check_strides("v", d->v, d->batch, d->kv_heads, d->n_k, d->head_dim, in, false)) != JV_OK) return st;
+    return diff_check_strides("o", d->o, d->batch, d->heads, d->n_q, d->head_dim, out, true);
+}
+
+static DiffPlan diff_plan_of(const jv_diff_attn_desc *d) {
+    return diff_plan(d->batch, d->kv_heads, (long long)d->heads / d->kv_heads * d->n_q, d->n_k);
+}
+
+size_t diff_saved_bytes(const jv_diff_attn_desc *d) {
+    const size_t rows = (size_t)d->batch * d->heads * d->n_q;
+    return ((rows * 8 + 255) & ~(size_t)255) + rows * d->head_dim * (d->dtype == JV_BF16 ? 2 : 4);
+}
+void diff_use_saved(DiffProblem *p, void *saved) {
+    const size_t rows = (size_t)diff_rows(p->a);
+    p->a.lse = (float *)saved;
+    p->a.o2 = (char *)saved + ((rows * 8 + 255) & ~(size_t)255);
+}
+
+jv_status diff_problem(const jv_diff_attn_desc *d, const void *q, const void *k, const void *v, void *o,
+                       const jv_diff_lambda *lambda, float scale, DiffProblem *p) {
+    jv_status st = diff_check_desc(d);
+    if (st != JV_OK) return st;
+    if (!q || !k || !v || !o) return fail(JV_ERR_INVALID_ARG, "q, k, v, o must be non-null");
+    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o) & 15) return fail(JV_ERR_INVALID_ARG, "q, k, v, o must be 16-byte aligned");
+    if (!lambda) return fail(JV_ERR_INVALID_ARG, "lambda is null");
+    if (!lambda->q1 || !lambda->k1 || !lambda->q2 || !lambda->k2) return fail(JV_ERR_INVALID_ARG, "lambda's vectors must be non-null");
+    if (((uintptr_t)lambda->q1 | (uintptr_t)lambda->k1 | (uintptr_t)lambda->q2 | (uintptr_t)lambda->k2) & 3)
+        return fail(JV_ERR_INVALID_ARG, "lambda's vectors must be 4-byte aligned");
+    if (!(fabsf(lambda->init) <= 3.4028235e38f)) return fail(JV_ERR_INVALID_ARG, "lambda's init must be finite");
+    if (scale > 3.4028235e38f) return fail(JV_ERR_INVALID_ARG, "scale must be finite");
+    *p = DiffProblem{};
+    DiffArgs &a = p->a;
+    a.B = d->batch;
+    a.heads = d->heads;
+    a.kv_heads = d->kv_heads;
+    a.group = d->heads / d->kv_heads;
+    a.n_q = d->n_q;
+    a.n_k = d->n_k;
+    a.causal = d->causal != 0;
+    a.q_len = d->q_lengths;
+    a.k_len = d->k_lengths;
+    a.scale = scale > 0.f ? scale : (float)(1.0 / sqrt(d->head_dim / 2.0));  // (NaN fails the comparison too)
+    a.c = a.scale * 1.4426950408889634f;
+    a.lq1 = lambda->q1;
+    a.lk1 = lambda->k1;
+    a.lq2 = lambda->q2;
+    a.lk2 = lambda->k2;
+    a.l_init = lambda->init;
+    a.l_step = lambda->per_head ? d->head_dim / 2 : 0;
+    auto arg = [](const void *ptr, const jv_strides &s) { return TensorArg{ptr, s.stride_b, s.stride_h, s.stride_n}; };
+    a.q = arg(q, d->q);
+    a.k = arg(k, d->k);
+    a.v = arg(v, d->v);
+    a.o = arg(o, d->o);
+    p->W = d->head_dim;
+    p->bf16 = d->dtype == JV_BF16;
+    p->o_bf16 = d->o_dtype == JV_BF16;
+    return JV_OK;
+}
+
+template <typename T, typename TO, int W>
+static jv_status diff_forward(DiffArgs a, const DiffPlan &plan, hipStream_t stream) {
+    a.blocks = plan.blocks;
+    a.splits = plan.splits;
+    a.tiles_per_split = plan.tiles_per_split;
+    a.items = (long long)a.B * a.kv_heads * a.blocks * a.splits;
+    const dim3 grid(diff_grid(a.items));
+    if (plan.splits == 1) {
+        if (plan.waves == 1) hipLaunchKernelGGL((diff_attn_fwd_kernel<T, TO, W, 1, false>), grid, dim3(64), 0, stream, a);
+        else hipLaunchKernelGGL((diff_attn_fwd_kernel<T, TO, W, 4, false>), grid, dim3(256), 0, stream, a);
+        return launch_status("diff_attn_fwd_kernel");
+    }
+    if (plan.waves == 1) hipLaunchKernelGGL((diff_attn_fwd_kernel<T, float, W, 1, true>), grid, dim3(64), 0, stream, a);
+    else hipLaunchKernelGGL((diff_attn_fwd_kernel<T, float, W, 4, true>), grid, dim3(256), 0, stream, a);
+    const jv_status st = launch_status("diff_attn_fwd_kernel");
+    if (st != JV_OK) return st;
+    hipLaunchKernelGGL((diff_attn_join_kernel<T, TO, W>), dim3((unsigned)((diff_rows(a) + 3) / 4)), dim3(256), 0, stream, a);
+    return launch_status("diff_attn_join_kernel");
+}
+
+}  // namespace jv
+
+extern "C" {
+
+size_t jv_diff_attn_workspace_bytes(const jv_diff_attn_desc *desc) {
+    jv::clear_error();
+    if (jv::diff_check_desc(desc) != JV_OK) return 0;
+    const size_t part = jv::diff_part_bytes(jv::diff_plan_of(desc), (long long)desc->batch * desc->heads * desc->n_q, desc->head_dim);
+    return part > 256 ? (part + 255) & ~(size_t)255 : 256;
+}
+
+size_t jv_diff_attn_saved_bytes(const jv_diff_attn_desc *desc) {
+    jv::clear_error();
+    return jv::diff_check_desc(desc) == JV_OK ? jv::diff_saved_bytes(desc) : 0;
+}
+
+jv_status jv_diff_attn_fwd(const jv_diff_attn_desc *desc, const void *q, const void *k, const void *v,
+                           const jv_diff_lambda *lambda, void *o, float scale, void *saved, size_t saved_bytes,
+                           void *workspace, size_t workspace_bytes, void *hip_stream) {
+    jv::clear_error();
+    jv::DiffProblem p;
+    jv_status st = jv::diff_problem(desc, q, k, v, o, lambda, scale, &p);
+    if (st != JV_OK) return st;
+    const int in = p.bf16 ? 2 : 4, out = p.o_bf16 ? 2 : 4;
+    const uintptr_t o0 = (uintptr_t)o, o1 = o0 + jv::diff_span(desc->o, desc->batch, desc->heads, desc->n_q, p.W) * out;
+    auto meets = [&](const void *ptr, int64_t bytes) { return o0 < (uintptr_t)ptr + bytes && (uintptr_t)ptr < o1; };
+    if (meets(q, jv::diff_span(desc->q, desc->batch, desc->heads, desc->n_q, p.W) * in) ||
+        meets(k, jv::diff_span(desc->k, desc->batch, desc->kv_heads, desc->n_k, p.W) * in) ||
+        meets(v, jv::diff_span(desc->v, desc->batch, desc->kv_heads, desc->n_k, p.W) * in))
+        return jv::fail(JV_ERR_INVALID_ARG, "o must not overlap an input");
+    if (saved) {
+        if ((uintptr_t)saved & 255) return jv::fail(JV_ERR_INVALID_ARG, "saved must be 256-byte aligned");
+        if (p.bf16 != p.o_bf16) return jv::fail(JV_ERR_UNSUPPORTED, "saved needs an output of the inputs' type");
+        if (saved_bytes < jv::diff_saved_bytes(desc))
+            return jv::fail(JV_ERR_WORKSPACE_TOO_SMALL, "saved holds %zu bytes, %zu are needed", saved_bytes, jv::diff_saved_bytes(desc));
+        jv::diff_use_saved(&p, saved);
+    }
+    const jv::DiffPlan plan = jv::diff_plan_of(desc);
+    const size_t need = jv_diff_attn_workspace_bytes(desc);
+    if (plan.splits > 1) {
+        if (!workspace) return jv::fail(JV_ERR_INVALID_ARG, "workspace must be non-null");
+        if ((uintptr_t)workspace & 255) return jv::fail(JV_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+        if (workspace_bytes < need) return jv::fail(JV_ERR_WORKSPACE_TOO_SMALL, "workspace holds %zu bytes, %zu are needed", workspace_bytes, need);
+        p.a.part = (float *)workspace;
+    }
+    if ((long long)desc->batch * desc->kv_heads * plan.blocks * plan.splits > 0x7ffffff0ll)
+        return jv::fail(JV_ERR_UNSUPPORTED, "more than 2^31 workgroups");
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    return jv::diff_with_kind(p.bf16, p.W, [&](auto kind) {
+        using K = decltype(kind);
+        if (p.o_bf16) {
+            if constexpr (sizeof(typename K::T) == 2) return jv::diff_forward<typename K::T, __bf16, K::W>(p.a, plan, stream);
+        }
+        return jv::diff_forward<typename K::T, float, K::W>(p.a, plan, stream);
+    });
+}
+
+}  // extern "C"

@@ -1,0 +1,164 @@
+"""Host-side checks of differential attention and of the gradients: what is refused before anything is launched, and the size queries."""
+import ctypes
+
+import pytest
+
+from paper_2605_26636_amd import binding
+
+INVALID, UNSUPPORTED, SMALL = binding.JV_ERR_INVALID_ARG, binding.JV_ERR_UNSUPPORTED, binding.JV_ERR_WORKSPACE_TOO_SMALL
+Q, K, V, O, SAVED, WORK, D_O, D_Q, D_K, D_V, VEC = (0x100000000 * (i + 1) for i in range(11))   # never dereferenced
+
+
+def strides(H, N, W):
+    return binding.JvStrides(H * N * W, N * W, W)
+
+
+def desc(B=2, H=4, G=2, n_q=50, n_k=60, W=64, dtype=binding.JV_BF16, o_dtype=None):
+    q, k = strides(H, n_q, W), strides(G, n_k, W)
+    return binding.JvDiffAttnDesc(B, H, G, n_q, n_k, W, dtype, dtype if o_dtype is None else o_dtype, q, k, k, q, 0, None, None)
+
+
+def lam(**change):
+    x = binding.JvDiffLambda(VEC, VEC, VEC, VEC, 0.5, 0)
+    for n, value in change.items():
+        setattr(x, n, value)
+    return x
+
+
+def forward(d, l=None, q=Q, k=K, v=V, o=O, scale=0.0, saved=None, saved_bytes=0, work=WORK, work_bytes=1 << 40):
+    L = binding.lib()
+    st = L.jv_diff_attn_fwd(None if d is None else ctypes.byref(d), q, k, v, ctypes.byref(l or lam()), o, scale, saved, saved_bytes, work, work_bytes, None)
+    assert st == binding.JV_OK or L.jv_last_error()
+    return st
+
+
+def grads(d, **change):
+    q, k = strides(d.heads, d.n_q, d.head_dim), strides(d.kv_heads, d.n_k, d.head_dim)
+    x = binding.JvDiffAttnGrads(D_O, D_Q, D_K, D_V, q, q, k, k, VEC, VEC, VEC, VEC)
+    for n, value in change.items():
+        setattr(x, n, value)
+    return x
+
+
+def backward(d, x=None, l=None, q=Q, k=K, v=V, o=O, scale=0.0, saved=SAVED, saved_bytes=1 << 40, work=WORK, work_bytes=1 << 40):
+    return binding.lib().jv_diff_attn_bwd(ctypes.byref(d), q, k, v, ctypes.byref(l or lam()), o, saved, saved_bytes, ctypes.byref(x or grads(d)), scale,
+                                          work, work_bytes, None)
+
+
+def queries(d):
+    return [f(d) for f in (binding.jv_diff_attn_workspace_bytes, binding.jv_diff_attn_saved_bytes, binding.jv_diff_attn_bwd_workspace_bytes)]
+
+
+BAD_FIELDS = [("batch", 0, INVALID), ("heads", -1, INVALID), ("kv_heads", 0, INVALID), ("kv_heads", 3, INVALID), ("n_q", 0, INVALID), ("n_k", 0, INVALID),
+              ("n_q", (1 << 24) + 1, UNSUPPORTED), ("n_k", (1 << 24) + 1, UNSUPPORTED), ("batch", 20000, UNSUPPORTED), ("head_dim", 0, INVALID),
+              ("head_dim", 32, UNSUPPORTED), ("head_dim", 256, UNSUPPORTED), ("dtype", 7, INVALID), ("o_dtype", 7, INVALID),
+              ("q_lengths", 2, INVALID), ("k_lengths", 5, INVALID)]
+
+
+@pytest.mark.parametrize("field,value,status", BAD_FIELDS)
+def test_descriptors_that_are_refused(field, value, status):
+    d = desc()
+    setattr(d, field, value)
+    assert forward(d) == status and backward(d) == status and queries(d) == [0, 0, 0]
+
+
+def test_strides_that_are_refused():
+    for name in "qkvo":
+        for field, value in (("stride_n", 32), ("stride_n", 66), ("stride_h", -64), ("stride_b", 1 << 62)):
+            d = desc()
+            setattr(getattr(d, name), field, value)
+            assert forward(d) == INVALID and backward(d) == INVALID and queries(d) == [0, 0, 0], (name, field)
+    d = desc()
+    d.o.stride_h = 0   # rows of O would lie on each other; K and V may be broadcast
+    assert forward(d) == INVALID
+    assert b"overlap" in binding.lib().jv_last_error()
+    d = desc()
+    d.k.stride_h = d.v.stride_h = d.v.stride_b = 0
+    assert all(queries(d))
+    d = desc(B=1, n_q=1)   # strides of axes of one are not used
+    d.q.stride_b, d.q.stride_n, d.o.stride_n, d.o.stride_b = -5, 3, 0, 7
+    assert all(queries(d))
+
+
+def test_pointers_and_lambda_that_are_refused():
+    d = desc()
+    assert forward(None) == INVALID
+    for name in "qkvo":
+        assert forward(d, **{name: None}) == INVALID and backward(d, **{name: None}) == INVALID
+        assert forward(d, **{name: 0x100000008}) == INVALID and backward(d, **{name: 0x100000008}) == INVALID
+    for change in (dict(q1=None), dict(k2=None), dict(k1=VEC + 2), dict(init=float("inf")), dict(init=float("nan"))):
+        assert forward(d, lam(**change)) == INVALID and backward(d, l=lam(**change)) == INVALID
+    assert binding.lib().jv_diff_attn_fwd(ctypes.byref(d), Q, K, V, None, O, 0.0, None, 0, WORK, 1 << 40, None) == INVALID
+    assert forward(d, scale=float("inf")) == INVALID
+    # O on an input, whole or by its last row
+    q_bytes, k_bytes = 2 * 2 * 4 * 50 * 64, 2 * 2 * 2 * 60 * 64
+    for at in (Q, Q + q_bytes - 16, K + k_bytes - 16, V, Q - q_bytes + 16):
+        assert forward(d, o=at) == INVALID
+        assert b"overlap" in binding.lib().jv_last_error()
+
+
+def test_types_saved_memory_and_workspaces_that_are_refused():
+    assert forward(desc(dtype=binding.JV_F32, o_dtype=binding.JV_BF16)) == UNSUPPORTED
+    mixed = desc(o_dtype=binding.JV_F32)
+    assert forward(mixed, saved=SAVED, saved_bytes=1 << 40) == UNSUPPORTED and backward(mixed) == UNSUPPORTED
+    for d in (desc(), desc(dtype=binding.JV_F32), desc(W=128)):
+        work, saved, back = queries(d)
+        rows, size = 2 * 4 * 50, 2 if d.dtype == binding.JV_BF16 else 4
+        assert saved >= rows * (8 + d.head_dim * size) and back >= rows * 8
+        assert forward(d, saved=SAVED, saved_bytes=saved - 1) == SMALL and forward(d, saved=SAVED + 16, saved_bytes=saved) == INVALID
+        assert backward(d, saved_bytes=saved - 1) == SMALL and backward(d, work_bytes=back - 1) == SMALL
+        assert backward(d, saved=None) == INVALID and backward(d, work=None) == INVALID and backward(d, work=WORK + 64) == INVALID
+    # few queries against many keys need room for parts
+    d = desc(n_q=1, n_k=5000)
+    assert queries(d)[0] > 256
+    assert forward(d, work=None) == INVALID and forward(d, work=WORK + 8) == INVALID and forward(d, work_bytes=queries(d)[0] - 1) == SMALL
+
+
+def test_gradients_that_are_refused():
+    d = desc()
+    for name in ("d_o", "d_q", "d_k", "d_v"):
+        assert backward(d, grads(d, **{name: None})) == INVALID and backward(d, grads(d, **{name: 0x700000004})) == INVALID
+    for name in ("d_q1", "d_k1", "d_q2", "d_k2"):
+        assert backward(d, grads(d, **{name: None})) == INVALID and backward(d, grads(d, **{name: VEC + 1})) == INVALID
+    for name, n in (("d_o", 4), ("d_q", 4), ("d_k", 2), ("d_v", 2)):
+        for field, value in (("stride_n", 8), ("stride_h", 50 * 64 + 4), ("stride_b", -64)):
+            x = grads(d)
+            setattr(getattr(x, name + "_strides"), field, value)
+            assert backward(d, x) == INVALID, (name, field)
+    for name in ("d_q", "d_k", "d_v"):   # rows that are written may not lie on each other
+        x = grads(d)
+        getattr(x, name + "_strides").stride_h = 0
+        assert backward(d, x) == INVALID
+        for at in (Q, K, V, O, D_O):
+            assert backward(d, grads(d, **{name: at})) == INVALID
+
+
+def norm(rows=10, cols=64, x=Q, gamma=VEC, dy=K, residual=None, dx=O, dgamma=D_Q, dbeta=D_K, eps=1e-6, x_type=0, dy_type=0, work=WORK, work_bytes=1 << 40):
+    return binding.lib().jv_layernorm_bwd(x, gamma, dy, residual, dx, dgamma, dbeta, rows, cols, eps, x_type, dy_type, work, work_bytes, None)
+
+
+def test_layernorm_gradients_that_are_refused():
+    assert binding.jv_layernorm_bwd_workspace_bytes(10, 64) > 0
+    for rows, cols, status in ((0, 64, INVALID), (-3, 64, INVALID), (5, 0, INVALID), (5, 12, UNSUPPORTED), (5, 8200, UNSUPPORTED), ((1 << 31) + 1, 8, UNSUPPORTED)):
+        assert norm(rows, cols) == status and binding.jv_layernorm_bwd_workspace_bytes(rows, cols) == 0
+    for name in ("x", "gamma", "dy", "dx"):
+        assert norm(**{name: None}) == INVALID and norm(**{name: 0x100000004}) == INVALID
+    assert norm(dgamma=None) == INVALID and norm(dbeta=None) == INVALID and norm(residual=V + 8) == INVALID
+    assert norm(eps=-1.0) == INVALID and norm(eps=float("nan")) == INVALID and norm(x_type=2) == INVALID and norm(dy_type=-1) == INVALID
+    assert norm(dx=Q) == INVALID and norm(dx=K + 10 * 64 * 4 - 16) == INVALID and norm(residual=V, dx=V + 256) == INVALID
+    assert norm(work=None) == INVALID and norm(work=WORK + 16) == INVALID
+    assert norm(work_bytes=binding.jv_layernorm_bwd_workspace_bytes(10, 64) - 1) == SMALL
+
+
+def test_binding_refuses_what_it_can_see():
+    torch = pytest.importorskip("torch")
+    q, k = torch.zeros(1, 2, 5, 64), torch.zeros(1, 1, 7, 64)
+    vec = tuple(torch.zeros(32) for _ in range(4))
+    with pytest.raises(ValueError):   # not on a GPU
+        binding.jv_diff_attn_fwd(q, k, k, vec, torch.zeros_like(q))
+    with pytest.raises(ValueError):
+        binding.jv_diff_attn_fwd(q, k, torch.zeros(1, 1, 8, 64), vec, torch.zeros_like(q))
+    with pytest.raises(TypeError):
+        binding.jv_diff_attn_fwd(q, k.bfloat16(), k, vec, torch.zeros_like(q))
+    with pytest.raises(ValueError):
+        binding.jv_layernorm_bwd(torch.zeros(4, 64), torch.zeros(64), torch.zeros(4, 64), torch.zeros(4, 64))
