@@ -152,26 +152,39 @@ struct DiffTile {
 };
 
 // A tile on its way from memory into LDS through the registers of THREADS threads: fetched while the tile before it is
-// worked on.  Rows at `limit` and beyond are not read and arrive as zeros.
+// worked on.  Rows at `limit` and beyond are not read and arrive as zeros.  The base of a piece is the same for all threads (scalar
+// registers), a thread's place in it a 32-bit offset: kDiffMostTokenStride elements from token to token at most.
+constexpr long long kDiffMostTokenStride = 1 << 25;
 template <typename T, int W, int THREADS>
 struct DiffFetch {
     using Tile = DiffTile<T, W>;
-    static constexpr int kPieces = kDiffTile * Tile::kChunks / THREADS;
-    static_assert(kPieces * THREADS == kDiffTile * Tile::kChunks, "whole pieces a thread");
+    static constexpr int kPieces = kDiffTile * Tile::kChunks / THREADS, kStep = THREADS / Tile::kChunks;  // rows from piece to piece
+    static_assert(kPieces * THREADS == kDiffTile * Tile::kChunks && kStep * Tile::kChunks == THREADS, "whole pieces a thread");
+    const char *base;
+    long long step;
+    unsigned at;
     u32x4 x[kPieces];
-    __device__ void fetch(const T *base, long long sn, int row0, int limit, int tid) {
+    __device__ void start(const void *tensor, long long offset, long long sn, int tid) {
+        base = (const char *)tensor + offset * (long long)sizeof(T);
+        step = sn * (long long)sizeof(T);
+        at = (unsigned)(tid / Tile::kChunks) * (unsigned)step + (tid % Tile::kChunks) * 16;
+    }
+    __device__ void fetch(int row0, int limit, int tid) {
+        const char *from = base + (long long)row0 * step;
+        if (row0 + kDiffTile <= limit) {  // (uniform)
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int p = tid + THREADS * i, row = row0 + p / Tile::kChunks;
-            x[i] = row < limit ? *(const u32x4 *)((const char *)(base + (long long)row * sn) + (p % Tile::kChunks) * 16) : u32x4{0, 0, 0, 0};
+            for (int i = 0; i < kPieces; ++i) x[i] = *(const u32x4 *)(from + i * kStep * step + at);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                x[i] = u32x4{0, 0, 0, 0};
+                if (row0 + i * kStep + tid / Tile::kChunks < limit) x[i] = *(const u32x4 *)(from + i * kStep * step + at);
+            }
         }
     }
     __device__ void store(unsigned char *tile, int tid) const {
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int p = tid + THREADS * i;
-            *(u32x4 *)(tile + Tile::off(p / Tile::kChunks, p % Tile::kChunks)) = x[i];
-        }
+        for (int i = 0; i < kPieces; ++i) *(u32x4 *)(tile + Tile::off(i * kStep + tid / Tile::kChunks, tid % Tile::kChunks)) = x[i];
     }
 };
 

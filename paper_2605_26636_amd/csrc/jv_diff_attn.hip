@@ -34,33 +34,36 @@ __device__ inline float diff_exp(f32x16 &p, const f32x16 &s, float c, float minu
     }
     return sum0 + sum1;
 }
-// Raises the reference to the tile's maximum and forms the weights against it from rounded products, whose maximum the
-// reference is (from exact ones a weight could be 2^(|m| 2^-24)).
+// Raises the reference to the tile's maximum; returns what the tile's weights are taken against.
 template <int W>
-__device__ inline float diff_raise(DiffMap<W> &w, f32x16 &p, const f32x16 &s, float c) {
-#pragma clang fp contract(off)
-    float t = s[0];
-#pragma unroll
-    for (int v = 1; v < 16; ++v) t = fmaxf(t, s[v]);
+__device__ inline float diff_raise(DiffMap<W> &w, const f32x16 &s, float c) {
+    const float t0 = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), t1 = fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7]));
+    const float t2 = fmaxf(fmaxf(s[8], s[9]), fmaxf(s[10], s[11])), t3 = fmaxf(fmaxf(s[12], s[13]), fmaxf(s[14], s[15]));
     float lo, hi;
-    pair_values(t * c, &lo, &hi);  // this lane and lane ^ 32 share the row
+    pair_values(fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * c, &lo, &hi);  // this lane and lane ^ 32 share the row
     const float m_new = fmaxf(w.m, fmaxf(lo, hi));
     const float alpha = w.m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(w.m - m_new);
     w.m = m_new;
     w.l *= alpha;
+    // In place, register by register, as an opaque instruction: the common path then needs no copies where the two paths meet.
+    // (alpha comes from a transcendental instruction, whose result the very next one may not read; inline assembly is not padded.)
+    asm volatile("s_nop 1" ::"v"(alpha));
 #pragma unroll
     for (int cb = 0; cb < W / 32; ++cb)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) w.acc[cb][v] *= alpha;
+        for (int v = 0; v < 16; ++v) {
+            float x = w.acc[cb][v];
+            asm volatile("v_mul_f32 %0, %0, %1" : "+v"(x) : "v"(alpha));
+            w.acc[cb][v] = x;
+        }
     w.minus_m = fabsf(m_new) < 16777216.f ? -m_new : INFINITY;  // (so large that products must be rounded first: no tile is tried; NaN too)
-    const float ref = m_new == -INFINITY ? 0.f : m_new;
-    float sum = 0.f;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-        p[v] = __builtin_amdgcn_exp2f(s[v] * c - ref);
-        sum += p[v];
-    }
-    return sum;
+    return m_new == -INFINITY ? 0.f : m_new;
+}
+// A weight from a rounded product, whose maximum the reference is (from an exact one it could be 2^(|m| 2^-24)).
+__device__ inline float diff_weight(float s, float c, float ref) {
+#pragma clang fp contract(off)
+    const float x = s * c;
+    return __builtin_amdgcn_exp2f(x - ref);
 }
 // Weights of a tile against the present reference, which is raised only where they come out large (numerator and denominator always
 // use the same one).  Without a reference minus_m is +inf, so every tile raises until a key is seen; where all is masked (s = -inf)
@@ -68,51 +71,134 @@ __device__ inline float diff_raise(DiffMap<W> &w, f32x16 &p, const f32x16 &s, fl
 template <int W>
 __device__ inline void diff_softmax(DiffMap<W> &w, f32x16 &p, const f32x16 &s, float c) {
     float sum = diff_exp(p, s, c, w.minus_m);
-    if (__builtin_amdgcn_ballot_w64(!(sum <= kDiffLazySum)) != 0) sum = diff_raise<W>(w, p, s, c);
+    if (__builtin_amdgcn_ballot_w64(!(sum <= kDiffLazySum)) != 0) {
+        const float ref = diff_raise<W>(w, s, c);
+        sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            p[v] = diff_weight(s[v], c, ref);
+            sum += p[v];
+        }
+    }
     w.l += sum;
 }
 
-// Rows of a (batch, kv head) are its group's heads one after the other, n_q queries each, so that a few queries of heads
-// that share K and V share a tile too.  WAVES x 32 rows a workgroup.
+// What a wavefront works on.  Rows of a (batch, kv head) are its group's heads one after the other, n_q queries each, so that a few queries of
+// heads that share K and V share a tile too; 32 rows a wavefront, a lane's row in lane % 32.
+struct DiffPlace {
+    int split, b, kv, bkv, n_rows, first, r, qi, head, limit;
+    bool row_live;
+    template <int WAVES, bool SPLIT>
+    __device__ bool find(const DiffArgs &a, int wave, int li) {
+        long long item = diff_item(a.items);
+        if (item >= a.items) return false;
+        split = SPLIT ? (int)(item % a.splits) : 0;
+        if (SPLIT) item /= a.splits;
+        const int block = a.blocks - 1 - (int)(item % a.blocks);  // causal: the longest rows first
+        bkv = (int)(item / a.blocks);
+        b = bkv / a.kv_heads;
+        kv = bkv % a.kv_heads;
+        n_rows = a.group * a.n_q;
+        first = (block * WAVES + wave) * 32;
+        r = first + li;
+        row_live = r < n_rows;
+        const int hg = row_live ? r / a.n_q : 0;
+        qi = row_live ? r - hg * a.n_q : 0;
+        head = kv * a.group + hg;
+        return true;
+    }
+};
+
+// Output of a wavefront's rows, or its part of it.
+template <typename T, typename TO, int W, bool SPLIT>
+__device__ inline void diff_finish(const DiffArgs &a, const DiffPlace &place, const DiffMap<W> &w1, const DiffMap<W> &w2, int lane) {
+    constexpr int CB = W / 32;
+    const int g = lane >> 5;
+    float lo, hi;
+    pair_values(w1.l, &lo, &hi);
+    const float l1 = lo + hi;
+    pair_values(w2.l, &lo, &hi);
+    const float l2 = lo + hi;
+    if (SPLIT) {
+        if (!place.row_live) return;
+        float *part = a.part + ((long long)place.split * a.B * a.kv_heads * place.n_rows + (long long)place.bkv * place.n_rows + place.r) * (2 * W + 4);
+        if (g == 0) *(f32x4 *)part = f32x4{w1.m, l1, w2.m, l2};
+        if (w1.m == -INFINITY && w2.m == -INFINITY) return;  // no key of this part is seen: not read again either
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                const f32x16 &x = w1.acc[cb], &y = w2.acc[cb];
+                *(f32x4 *)(part + 4 + 32 * cb + 8 * q4 + 4 * g) = f32x4{x[4 * q4], x[4 * q4 + 1], x[4 * q4 + 2], x[4 * q4 + 3]};
+                *(f32x4 *)(part + 4 + W + 32 * cb + 8 * q4 + 4 * g) = f32x4{y[4 * q4], y[4 * q4 + 1], y[4 * q4 + 2], y[4 * q4 + 3]};
+            }
+        return;
+    }
+    float lam = 0.f;
+    for (int h = __builtin_amdgcn_readfirstlane(place.head), last = place.kv * a.group + min(place.first + 31, place.n_rows - 1) / a.n_q; h <= last; ++h) {
+        const float x = diff_lambda<W>(a, h, lane).value;
+        if (place.head == h) lam = x;
+    }
+    if (!place.row_live) return;
+    const float inv1 = l1 > 0.f ? 1.f / l1 : l1, inv2 = l2 > 0.f ? 1.f / l2 : l2;  // (0 for a row that sees nothing, NaN stays NaN)
+    const long long row = ((long long)place.b * a.heads + place.head) * a.n_q + place.qi;
+    if (a.lse && g == 0) {
+        a.lse[row] = w1.m == -INFINITY ? INFINITY : w1.m + log2f(l1);
+        a.lse[diff_rows(a) + row] = w2.m == -INFINITY ? INFINITY : w2.m + log2f(l2);
+    }
+    TO *o = (TO *)const_cast<void *>(a.o.ptr) + place.b * a.o.sb + place.head * a.o.sh + place.qi * a.o.sn;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+            const int ch = 32 * cb + 8 * q4 + 4 * g;
+            f32x4 x, y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                y[e] = w2.acc[cb][4 * q4 + e] * inv2;
+                x[e] = fmaf(-lam, y[e], w1.acc[cb][4 * q4 + e] * inv1);
+            }
+            diff_store4(o + ch, x);
+            if (a.o2) diff_store4((T *)a.o2 + row * W + ch, y);
+        }
+}
+
+// WAVES x 32 rows a workgroup.
 // SPLIT: a workgroup takes a part of the keys and leaves (m, l) of both maps and the unnormalised outputs in a.part.
-template <typename T, typename TO, int W, int WAVES, bool SPLIT>
-__global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 2 : 1) diff_attn_fwd_kernel(DiffArgs a) {
+template <int W, int WAVES, bool SPLIT>
+__global__ void __launch_bounds__(64 * WAVES, 1) diff_attn_fwd_f32_kernel(DiffArgs a) {
+    using T = float;
     using Tile = DiffTile<T, W>;
     constexpr int THREADS = 64 * WAVES, KS = W / 16, CB = W / 32;
     __shared__ __align__(16) unsigned char smem[2][2][Tile::kBytes];
     __shared__ int wave_most[WAVES];
-    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = tid >> 6;
-    long long item = diff_item(a.items);
-    if (item >= a.items) return;  // whole workgroup
-    const int split = SPLIT ? (int)(item % a.splits) : 0;
-    if (SPLIT) item /= a.splits;
-    const int block = a.blocks - 1 - (int)(item % a.blocks);  // causal: the longest rows first
-    const int bkv = (int)(item / a.blocks), b = bkv / a.kv_heads, kv = bkv % a.kv_heads;
-    const DiffLengths len(a, b);
-
-    const int n_rows = a.group * a.n_q, r = (block * WAVES + wave) * 32 + li;
-    const bool row_live = r < n_rows;
-    const int hg = row_live ? r / a.n_q : 0, qi = row_live ? r - hg * a.n_q : 0, head = kv * a.group + hg;
-    const int limit = row_live ? len.limit(a, qi) : 0;
-    int most = limit, least = row_live ? limit : a.n_k;
+    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    DiffPlace place;
+    if (!place.find<WAVES, SPLIT>(a, wave, li)) return;  // whole workgroup
+    const DiffLengths len(a, place.b);
+    const int limit = place.row_live ? len.limit(a, place.qi) : 0;
+    int most = limit, least = place.row_live ? limit : a.n_k;
 #pragma unroll
     for (int x = 1; x < 32; x *= 2) {
         most = max(most, __shfl_xor(most, x));
         least = min(least, __shfl_xor(least, x));
     }
+    most = __builtin_amdgcn_readfirstlane(most);
+    least = __builtin_amdgcn_readfirstlane(least);
     int wg_most = most;
     if (WAVES > 1) {
         if (lane == 0) wave_most[wave] = most;
         __syncthreads();
 #pragma unroll
         for (int x = 0; x < WAVES; ++x) wg_most = max(wg_most, wave_most[x]);
+        wg_most = __builtin_amdgcn_readfirstlane(wg_most);
     }
-    int tile = SPLIT ? split * a.tiles_per_split : 0, tile_end = (wg_most + kDiffTile - 1) / kDiffTile;
+    int tile = SPLIT ? place.split * a.tiles_per_split : 0, tile_end = (wg_most + kDiffTile - 1) / kDiffTile;
     if (SPLIT) tile_end = min(tile_end, tile + a.tiles_per_split);
 
     DiffFrag<T> q[KS];
     {
-        const T *row = (const T *)a.q.ptr + b * a.q.sb + head * a.q.sh + qi * a.q.sn;
+        const T *row = (const T *)a.q.ptr + place.b * a.q.sb + place.head * a.q.sh + place.qi * a.q.sn;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) q[ks] = diff_global_frag<T>(row, ks, g, limit > 0);
     }
@@ -126,11 +212,12 @@ __global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 2 : 1) diff_attn_
         diff_zero(w2.acc[cb]);
     }
 
-    const T *kbase = (const T *)a.k.ptr + b * a.k.sb + kv * a.k.sh, *vbase = (const T *)a.v.ptr + b * a.v.sb + kv * a.v.sh;
     DiffFetch<T, W, THREADS> kf, vf;
+    kf.start(a.k.ptr, place.b * a.k.sb + place.kv * a.k.sh, a.k.sn, tid);
+    vf.start(a.v.ptr, place.b * a.v.sb + place.kv * a.v.sh, a.v.sn, tid);
     auto fetch = [&](int t) {
-        kf.fetch(kbase, a.k.sn, t * kDiffTile, len.k, tid);
-        vf.fetch(vbase, a.v.sn, t * kDiffTile, len.k, tid);
+        kf.fetch(t * kDiffTile, len.k, tid);
+        vf.fetch(t * kDiffTile, len.k, tid);
     };
     if (tile < tile_end) {
         fetch(tile);
@@ -138,7 +225,8 @@ __global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 2 : 1) diff_attn_
         vf.store(smem[0][1], tid);
     }
     lds_barrier();
-    for (int at = 0; tile < tile_end; ++tile, at ^= 1) {
+    auto step = [&](auto buffer) {
+        constexpr int at = decltype(buffer)::value;
         const bool more = tile + 1 < tile_end;
         if (more) fetch(tile + 1);
         if (tile * kDiffTile < most) {  // (uniform in the wavefront)
@@ -182,55 +270,262 @@ __global__ void __launch_bounds__(64 * WAVES, sizeof(T) == 2 ? 2 : 1) diff_attn_
             vf.store(smem[at ^ 1][1], tid);
         }
         lds_barrier();
+    };
+    while (tile < tile_end) {  // (one copy of the tile for each buffer, whose place is then part of the instructions)
+        step(std::integral_constant<int, 0>());
+        if (++tile >= tile_end) break;
+        step(std::integral_constant<int, 1>());
+        ++tile;
     }
+    diff_finish<float, float, W, SPLIT>(a, place, w1, w2, lane);
+}
 
-    float lo, hi;
-    pair_values(w1.l, &lo, &hi);
-    const float l1 = lo + hi;
-    pair_values(w2.l, &lo, &hi);
-    const float l2 = lo + hi;
-    if (SPLIT) {
-        if (!row_live) return;
-        float *part = a.part + ((long long)split * a.B * a.kv_heads * n_rows + (long long)bkv * n_rows + r) * (2 * W + 4);
-        if (g == 0) *(f32x4 *)part = f32x4{w1.m, l1, w2.m, l2};
-        if (w1.m == -INFINITY && w2.m == -INFINITY) return;  // no key of this part is seen: not read again either
+// ---------------------------------------------------------------------------------------
+// bf16 tensors.  As diff_attn_fwd_f32_kernel, with the tiles brought from memory straight into a ring of three LDS stages, two
+// tiles ahead, and LDS read in assembly with waits of its own (the compiler would wait for every load into LDS in front of
+// a read, and has no registers left for tiles on their way).  A tile: first map's scores on K operands that were read at the end of
+// the tile before, second map's operands meanwhile; the hand-over of the stages; V operands of 16 keys, under whose latency
+// both softmaxes run; the products with V, the next 16 keys' operands and then the next tile's K operands in flight.
+// Rows behind the last key are fetched as the last one, which is masked there.  Rows that see no key go along unmasked and are
+// dropped at the end.
+// ---------------------------------------------------------------------------------------
+typedef __attribute__((address_space(3))) void diff_lds_void;
+typedef const __attribute__((address_space(1))) void diff_global_cvoid;
+
+__device__ inline void diff_landed(u32x4 (&x)[4]) {
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));
+}
+__device__ inline void diff_landed(u32x4 (&x)[2]) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1])); }
+__device__ inline void diff_landed(u32x2 (&x)[8]) {
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]), "+v"(x[7]));
+}
+__device__ inline void diff_landed(u32x2 (&x)[4]) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3])); }
+
+// Layouts of a stage: K rows for row-per-lane reads, V rows for transposing ones (rows 8 apart are moved alike).
+template <int W>
+struct DiffStage {
+    static constexpr int kRow = 2 * W, kTile = kDiffTile * kRow, kBytes = 2 * kTile, kChunks = W / 8, kRing = 3;
+    __device__ static unsigned k_off(int row, int chunk) { return W == 128 ? wide_off_row(row, chunk) : tile_off_row(row, chunk); }
+    __device__ static unsigned v_off(int row, int chunk) { return W == 128 ? wide_off_tr(row, chunk) : tile_off_tr(row, chunk); }
+    // What 16-byte slot `slot` of a row holds (both layouts move chunks by exclusive or: its own inverse).
+    __device__ static unsigned k_chunk(int row, int slot) { return (k_off(row, slot) - row * kRow) / 16; }
+    __device__ static unsigned v_chunk(int row, int slot) { return (v_off(row, slot) - row * kRow) / 16; }
+};
+
+// Weights of a tile packed to bf16, and the running softmax: see diff_softmax.
+__device__ inline float diff_exp_pack(unsigned (&pk)[8], const f32x16 &s, float c, float minus_m) {
+    float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+    for (int v = 0; v < 8; ++v) {
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(s[2 * v], c, minus_m)), p1 = __builtin_amdgcn_exp2f(fmaf(s[2 * v + 1], c, minus_m));
+        pk[v] = pack_bf16x2(p0, p1);
+        sum0 += p0;
+        sum1 += p1;
+    }
+    return sum0 + sum1;
+}
+template <int W>
+__device__ inline void diff_softmax_pack(DiffMap<W> &w, unsigned (&pk)[8], const f32x16 &s, float c) {
+    float sum = diff_exp_pack(pk, s, c, w.minus_m);
+    if (__builtin_amdgcn_ballot_w64(!(sum <= kDiffLazySum)) != 0) {
+        const float ref = diff_raise<W>(w, s, c);
+        sum = 0.f;
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+            const float p0 = diff_weight(s[2 * v], c, ref), p1 = diff_weight(s[2 * v + 1], c, ref);
+            pk[v] = pack_bf16x2(p0, p1);
+            sum += p0 + p1;
+        }
+    }
+    w.l += sum;
+}
+
+template <typename TO, int W, int WAVES, bool SPLIT>
+__global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffArgs a) {
+    using Stage = DiffStage<W>;
+    constexpr int KS = W / 32, CB = W / 32;           // steps of 16 channels of a map; blocks of 32 channels
+    constexpr int LOADS = kDiffTile * W / (512 * WAVES);  // instructions of 1 KB a wavefront and tile of K or V
+    constexpr int LOAD_ROWS = 512 / W;                // rows of one
+    __shared__ __align__(1024) unsigned char smem[Stage::kRing * Stage::kBytes];
+    __shared__ int wave_most[WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    DiffPlace place;
+    if (!place.find<WAVES, SPLIT>(a, wave, li)) return;  // whole workgroup
+    const DiffLengths len(a, place.b);
+    const int sees = place.row_live ? len.limit(a, place.qi) : 0, limit = sees > 0 ? sees : a.n_k + kDiffTile;
+    int most = sees, least = limit;
+#pragma unroll
+    for (int x = 1; x < 32; x *= 2) {
+        most = max(most, __shfl_xor(most, x));
+        least = min(least, __shfl_xor(least, x));
+    }
+    least = __builtin_amdgcn_readfirstlane(least);
+    if (WAVES > 1) {
+        if (lane == 0) wave_most[wave] = most;
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < WAVES; ++x) most = max(most, wave_most[x]);
+    }
+    most = __builtin_amdgcn_readfirstlane(most);
+    int tile = SPLIT ? place.split * a.tiles_per_split : 0, tile_end = (most + kDiffTile - 1) / kDiffTile;
+    if (SPLIT) tile_end = min(tile_end, tile + a.tiles_per_split);
+
+    // Loads of a tile: a wavefront's instructions cover LOAD_ROWS rows each; a lane fetches the chunk that belongs in its slot.
+    auto uniform = [](const void *ptr) {
+        const unsigned long long u = (unsigned long long)ptr;
+        const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)u), hi = __builtin_amdgcn_readfirstlane((unsigned)(u >> 32));
+        return (const char *)((unsigned long long)hi << 32 | lo);
+    };
+    const char *kbase = uniform((const __bf16 *)a.k.ptr + place.b * a.k.sb + place.kv * a.k.sh);
+    const char *vbase = uniform((const __bf16 *)a.v.ptr + place.b * a.v.sb + place.kv * a.v.sh);
+    const long long kstep = 2 * a.k.sn, vstep = 2 * a.v.sn;  // bytes from token to token
+    const int load_row = lane / Stage::kChunks, slot = lane % Stage::kChunks;
+    unsigned koff[LOADS], voff[LOADS];  // bytes from the tile's token of the instruction's first row
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int row = (wave * LOADS + i) * LOAD_ROWS + load_row;
+        koff[i] = (unsigned)load_row * (unsigned)kstep + 16 * Stage::k_chunk(row, slot);
+        voff[i] = (unsigned)load_row * (unsigned)vstep + 16 * Stage::v_chunk(row, slot);
+    }
+    auto issue = [&](int t, int to) {
+        unsigned char *kt = smem + to * Stage::kBytes, *vt = kt + Stage::kTile;
+        const char *kp = kbase + t * kDiffTile * kstep, *vp = vbase + t * kDiffTile * vstep;
+        if ((t + 1) * kDiffTile <= len.k) {  // (uniform)
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int row0 = (wave * LOADS + i) * LOAD_ROWS;
+                __builtin_amdgcn_global_load_lds((diff_global_cvoid *)(kp + row0 * kstep + koff[i]), (diff_lds_void *)(kt + row0 * Stage::kRow), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((diff_global_cvoid *)(vp + row0 * vstep + voff[i]), (diff_lds_void *)(vt + row0 * Stage::kRow), 16, 0, 0);
+            }
+        } else {
+            int l = lane;
+            asm("" : "+v"(l));  // (worked out here: in registers all the way they would be missed)
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int row0 = (wave * LOADS + i) * LOAD_ROWS, row = row0 + l / Stage::kChunks;
+                const unsigned from = (unsigned)min(row, len.k - 1 - t * kDiffTile);
+                __builtin_amdgcn_global_load_lds((diff_global_cvoid *)(kp + (from * (unsigned)kstep + 16 * Stage::k_chunk(row, l % Stage::kChunks))), (diff_lds_void *)(kt + row0 * Stage::kRow), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((diff_global_cvoid *)(vp + (from * (unsigned)vstep + 16 * Stage::v_chunk(row, l % Stage::kChunks))), (diff_lds_void *)(vt + row0 * Stage::kRow), 16, 0, 0);
+            }
+        }
+    };
+    DiffFrag<__bf16> q[2 * KS];
+    {
+        const __bf16 *row = (const __bf16 *)a.q.ptr + place.b * a.q.sb + place.head * a.q.sh + place.qi * a.q.sn;
+#pragma unroll
+        for (int ks = 0; ks < 2 * KS; ++ks) q[ks] = diff_global_frag<__bf16>(row, ks, g, sees > 0);
+    }
+    if (tile < tile_end) issue(tile, 0);
+    if (tile + 1 < tile_end) issue(tile + 1, 1);
+
+    DiffMap<W> w1, w2;
+    w1.m = w2.m = -INFINITY;
+    w1.minus_m = w2.minus_m = INFINITY;
+    w1.l = w2.l = 0.f;
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+        diff_zero(w1.acc[cb]);
+        diff_zero(w2.acc[cb]);
+    }
+    // Operand addresses of stage 0; a K operand's chunk 2 ks + g is exclusive-or'ed with 2 ks (formed at the read: one register).
+    unsigned kaddr = lds_address(smem) + Stage::k_off(li, g), vaddr[CB];
+    {
+        const int blk = lane >> 4, j = lane & 15;
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4) {
-                const f32x16 &x = w1.acc[cb], &y = w2.acc[cb];
-                *(f32x4 *)(part + 4 + 32 * cb + 8 * q4 + 4 * g) = f32x4{x[4 * q4], x[4 * q4 + 1], x[4 * q4 + 2], x[4 * q4 + 3]};
-                *(f32x4 *)(part + 4 + W + 32 * cb + 8 * q4 + 4 * g) = f32x4{y[4 * q4], y[4 * q4 + 1], y[4 * q4 + 2], y[4 * q4 + 3]};
-            }
-        return;
+            vaddr[cb] = lds_address(smem) + Stage::kTile + Stage::v_off(4 * g + (j >> 2), cb * 4 + (blk & 1) * 2 + ((j & 3) >> 1)) + (j & 1) * 8;
     }
-    float lam = 0.f;
-    for (int h = __builtin_amdgcn_readfirstlane(head), last = kv * a.group + min((block * WAVES + wave) * 32 + 31, n_rows - 1) / a.n_q; h <= last; ++h) {
-        const float x = diff_lambda<W>(a, h, lane).value;
-        if (head == h) lam = x;
+    u32x4 k1[KS];
+    if (tile < tile_end) {
+#pragma unroll
+        for (int ks = 0; ks < 2 * KS; ++ks) asm volatile("" : "+v"(q[ks].x));  // (waited for here, not inside the loop)
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        lds_barrier();
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) k1[ks] = lds_read_b128_at<0>(kaddr ^ 32 * ks);
+        diff_landed(k1);
     }
-    if (!row_live) return;
-    const float inv1 = l1 > 0.f ? 1.f / l1 : l1, inv2 = l2 > 0.f ? 1.f / l2 : l2;  // (0 for a row that sees nothing, NaN stays NaN)
-    const long long row = ((long long)b * a.heads + head) * a.n_q + qi;
-    if (a.lse && g == 0) {
-        a.lse[row] = w1.m == -INFINITY ? INFINITY : w1.m + log2f(l1);
-        a.lse[diff_rows(a) + row] = w2.m == -INFINITY ? INFINITY : w2.m + log2f(l2);
-    }
-    TO *o = (TO *)const_cast<void *>(a.o.ptr) + b * a.o.sb + head * a.o.sh + qi * a.o.sn;
+    for (int stage = 0; tile < tile_end; ++tile) {
+        const int next = stage + 1 == Stage::kRing ? 0 : stage + 1, after = next + 1 == Stage::kRing ? 0 : next + 1;
+        const unsigned kat = kaddr + stage * Stage::kBytes, vat = stage * Stage::kBytes;
+        f32x16 s1, s2;
+        diff_zero(s1);
+        diff_zero(s2);
+        u32x4 k2[KS];
 #pragma unroll
-    for (int cb = 0; cb < CB; ++cb)
+        for (int ks = 0; ks < KS; ++ks) k2[ks] = lds_read_b128_at<0>(kat ^ 32 * (KS + ks));
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-            const int ch = 32 * cb + 8 * q4 + 4 * g;
-            f32x4 x, y;
+        for (int ks = 0; ks < KS; ++ks) s1 = mfma32(as_bf16x8(k1[ks]), q[ks].x, s1);
+        diff_landed(k2);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                y[e] = w2.acc[cb][4 * q4 + e] * inv2;
-                x[e] = fmaf(-lam, y[e], w1.acc[cb][4 * q4 + e] * inv1);
-            }
-            diff_store4(o + ch, x);
-            if (a.o2) diff_store4((T *)a.o2 + row * W + ch, y);
+        for (int ks = 0; ks < KS; ++ks) s2 = mfma32(as_bf16x8(k2[ks]), q[KS + ks].x, s2);
+        __builtin_amdgcn_sched_barrier(0);
+        // the next tile has landed for every wavefront, and every wavefront has left the tile before, whose stage takes the one after
+        if (tile + 1 < tile_end) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            lds_barrier();
+            if (tile + 2 < tile_end) issue(tile + 2, after);
         }
+        if ((tile + 1) * kDiffTile > least) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const bool hidden = tile * kDiffTile + 8 * (v / 4) + 4 * g + v % 4 >= limit;
+                s1[v] = hidden ? -INFINITY : s1[v];
+                s2[v] = hidden ? -INFINITY : s2[v];
+            }
+        }
+        unsigned p1[8], p2[8];
+        diff_softmax_pack<W>(w1, p1, s1, a.c);
+        u32x2 v0[2 * CB];
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            v0[2 * cb] = lds_read_tr16_at<0>(vaddr[cb] + vat);
+            v0[2 * cb + 1] = lds_read_tr16_at<8 * Stage::kRow>(vaddr[cb] + vat);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        diff_softmax_pack<W>(w2, p2, s2, a.c);
+        auto products = [&](const u32x2 (&v)[2 * CB], int kk) {
+            const bf16x8 b1 = as_bf16x8(u32x4{p1[4 * kk], p1[4 * kk + 1], p1[4 * kk + 2], p1[4 * kk + 3]});
+            const bf16x8 b2 = as_bf16x8(u32x4{p2[4 * kk], p2[4 * kk + 1], p2[4 * kk + 2], p2[4 * kk + 3]});
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) {
+                const bf16x8 x = as_bf16x8(u32x4{v[2 * cb][0], v[2 * cb][1], v[2 * cb + 1][0], v[2 * cb + 1][1]});
+                w1.acc[cb] = mfma32(x, b1, w1.acc[cb]);
+                w2.acc[cb] = mfma32(x, b2, w2.acc[cb]);
+            }
+        };
+        diff_landed(v0);
+        u32x2 v1[2 * CB];
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            v1[2 * cb] = lds_read_tr16_at<16 * Stage::kRow>(vaddr[cb] + vat);
+            v1[2 * cb + 1] = lds_read_tr16_at<24 * Stage::kRow>(vaddr[cb] + vat);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        products(v0, 0);
+        diff_landed(v1);
+        // (after the last tile: of a stage that nobody needs)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) k1[ks] = lds_read_b128_at<0>((kaddr + next * Stage::kBytes) ^ 32 * ks);
+        __builtin_amdgcn_sched_barrier(0);
+        products(v1, 1);
+        diff_landed(k1);
+        stage = next;
+    }
+    int l = lane;
+    asm("" : "+v"(l));  // (where the rows lie is worked out again: kept across the loop it would cost registers that are missed there)
+    place.find<WAVES, SPLIT>(a, wave, l & 31);
+    if ((place.row_live ? len.limit(a, place.qi) : 0) == 0) {
+        w1.m = w2.m = -INFINITY;
+        w1.l = w2.l = 0.f;
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) {
+            diff_zero(w1.acc[cb]);
+            diff_zero(w2.acc[cb]);
+        }
+    }
+    diff_finish<__bf16, TO, W, SPLIT>(a, place, w1, w2, l);
 }
 
 // The parts of a row joined, in their order: one wavefront a row.
@@ -313,6 +608,7 @@ jv_status diff_check_strides(const char *name, const jv_strides &s, int64_t b, i
     for (int i = 0; i < 3; ++i) {
         if (size[i] == 1) continue;  // the stride of an axis of one is not used
         if (stride[i] < 0) return fail(JV_ERR_INVALID_ARG, "%s: negative stride", name);
+        if (i == 2 && stride[i] > kDiffMostTokenStride) return fail(JV_ERR_UNSUPPORTED, "%s: stride_n above 2^25", name);
         if (i == 2 && stride[i] < W) return fail(JV_ERR_INVALID_ARG, "%s: stride_n < head_dim", name);
         if (stride[i] % align) return fail(JV_ERR_INVALID_ARG, "%s: strides must keep rows 16-byte aligned", name);
         if (stride[i] > (INT64_C(1) << 56) / size[i]) return fail(JV_ERR_INVALID_ARG, "%s: strides reach beyond the address space", name);
@@ -421,13 +717,20 @@ static jv_status diff_forward(DiffArgs a, const DiffPlan &plan, hipStream_t stre
     a.tiles_per_split = plan.tiles_per_split;
     a.items = (long long)a.B * a.kv_heads * a.blocks * a.splits;
     const dim3 grid(diff_grid(a.items));
+    auto launch = [&](auto waves, auto split) {
+        constexpr int WAVES = decltype(waves)::value;
+        constexpr bool SPLIT = decltype(split)::value;
+        using Out = std::conditional_t<SPLIT, float, TO>;
+        if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((diff_attn_fwd_bf16_kernel<Out, W, WAVES, SPLIT>), grid, dim3(64 * WAVES), 0, stream, a);
+        else hipLaunchKernelGGL((diff_attn_fwd_f32_kernel<W, WAVES, SPLIT>), grid, dim3(64 * WAVES), 0, stream, a);
+    };
     if (plan.splits == 1) {
-        if (plan.waves == 1) hipLaunchKernelGGL((diff_attn_fwd_kernel<T, TO, W, 1, false>), grid, dim3(64), 0, stream, a);
-        else hipLaunchKernelGGL((diff_attn_fwd_kernel<T, TO, W, 4, false>), grid, dim3(256), 0, stream, a);
+        if (plan.waves == 1) launch(std::integral_constant<int, 1>(), std::false_type());
+        else launch(std::integral_constant<int, 4>(), std::false_type());
         return launch_status("diff_attn_fwd_kernel");
     }
-    if (plan.waves == 1) hipLaunchKernelGGL((diff_attn_fwd_kernel<T, float, W, 1, true>), grid, dim3(64), 0, stream, a);
-    else hipLaunchKernelGGL((diff_attn_fwd_kernel<T, float, W, 4, true>), grid, dim3(256), 0, stream, a);
+    if (plan.waves == 1) launch(std::integral_constant<int, 1>(), std::true_type());
+    else launch(std::integral_constant<int, 4>(), std::true_type());
     const jv_status st = launch_status("diff_attn_fwd_kernel");
     if (st != JV_OK) return st;
     hipLaunchKernelGGL((diff_attn_join_kernel<T, TO, W>), dim3((unsigned)((diff_rows(a) + 3) / 4)), dim3(256), 0, stream, a);

@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) diff_attn_dq_kern
     __shared__ __align__(16) unsigned char smem[2][2][Tile::kBytes];
     __shared__ int wave_most[4];
     __shared__ float wave_lam[4];
-    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const long long item = diff_item(a.items);
     if (item >= a.items) return;  // whole workgroup
     const int block = a.blocks - 1 - (int)(item % a.blocks), bh = (int)(item / a.blocks), b = bh / a.heads, h = bh % a.heads, kv = h / a.group;
@@ -83,7 +83,10 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) diff_attn_dq_kern
     }
     if (lane == 0) wave_most[wave] = most;
     __syncthreads();
-    const int tile_end = (max(max(wave_most[0], wave_most[1]), max(wave_most[2], wave_most[3])) + kDiffTile - 1) / kDiffTile;
+    most = __builtin_amdgcn_readfirstlane(most);
+    least = __builtin_amdgcn_readfirstlane(least);
+    const int wg_most = __builtin_amdgcn_readfirstlane(max(max(wave_most[0], wave_most[1]), max(wave_most[2], wave_most[3])));
+    const int tile_end = (wg_most + kDiffTile - 1) / kDiffTile;
     const float lam = diff_lambda<W>(a, h, lane).value;
 
     DiffFrag<T> q[KS], go[KS];
@@ -104,20 +107,23 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) diff_attn_dq_kern
     for (int cb = 0; cb < CB; ++cb) diff_zero(acc[cb]);
     float lam_sum = 0.f;
 
-    const T *kbase = (const T *)a.k.ptr + b * a.k.sb + kv * a.k.sh, *vbase = (const T *)a.v.ptr + b * a.v.sb + kv * a.v.sh;
     DiffFetch<T, W, 256> kf, vf;
+    kf.start(a.k.ptr, b * a.k.sb + kv * a.k.sh, a.k.sn, tid);
+    vf.start(a.v.ptr, b * a.v.sb + kv * a.v.sh, a.v.sn, tid);
     if (tile_end > 0) {
-        kf.fetch(kbase, a.k.sn, 0, len.k, tid);
-        vf.fetch(vbase, a.v.sn, 0, len.k, tid);
+        kf.fetch(0, len.k, tid);
+        vf.fetch(0, len.k, tid);
         kf.store(smem[0][0], tid);
         vf.store(smem[0][1], tid);
     }
     lds_barrier();
-    for (int tile = 0, at = 0; tile < tile_end; ++tile, at ^= 1) {
+    int tile = 0;
+    auto step = [&](auto buffer) {
+        constexpr int at = decltype(buffer)::value;
         const bool more = tile + 1 < tile_end;
         if (more) {
-            kf.fetch(kbase, a.k.sn, (tile + 1) * kDiffTile, len.k, tid);
-            vf.fetch(vbase, a.v.sn, (tile + 1) * kDiffTile, len.k, tid);
+            kf.fetch((tile + 1) * kDiffTile, len.k, tid);
+            vf.fetch((tile + 1) * kDiffTile, len.k, tid);
         }
         if (tile * kDiffTile < most) {  // (uniform in the wavefront)
             const unsigned char *kt = smem[at][0], *vt = smem[at][1];
@@ -160,6 +166,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) diff_attn_dq_kern
             vf.store(smem[at ^ 1][1], tid);
         }
         lds_barrier();
+    };
+    while (tile < tile_end) {  // (one copy of the tile for each buffer)
+        step(std::integral_constant<int, 0>());
+        if (++tile >= tile_end) break;
+        step(std::integral_constant<int, 1>());
+        ++tile;
     }
     if (row_live) {
         T *dq = (T *)const_cast<void *>(a.dq.ptr) + b * a.dq.sb + h * a.dq.sh + qi * a.dq.sn;
@@ -187,7 +199,7 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_kernel(DiffArgs a) {
     constexpr int KS = W / 16, CB = W / 32;
     __shared__ __align__(16) unsigned char smem[2][2][Tile::kBytes];
     __shared__ __align__(16) float stats[2][4][kDiffTile];  // of a tile's queries: both denominators, D1, D2
-    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const long long item = diff_item(a.items);
     if (item >= a.items) return;  // whole workgroup
     const int block = (int)(item % a.blocks), bkv = (int)(item / a.blocks), b = bkv / a.kv_heads, kv = bkv % a.kv_heads;
@@ -219,13 +231,14 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_kernel(DiffArgs a) {
     for (int hg = 0; hg < (n_tiles ? a.group : 0); ++hg) {
         const int h = kv * a.group + hg;
         const float lam = diff_lambda<W>(a, h, lane).value;
-        const T *qbase = (const T *)a.q.ptr + b * a.q.sb + h * a.q.sh, *gbase = (const T *)a.d_o.ptr + b * a.d_o.sb + h * a.d_o.sh;
         const long long row0 = ((long long)b * a.heads + h) * a.n_q;
         DiffFetch<T, W, 256> qf, gf;
+        qf.start(a.q.ptr, b * a.q.sb + h * a.q.sh, a.q.sn, tid);
+        gf.start(a.d_o.ptr, b * a.d_o.sb + h * a.d_o.sh, a.d_o.sn, tid);
         float stat = 0.f;
         auto fetch = [&](int tile) {
-            qf.fetch(qbase, a.q.sn, tile * kDiffTile, len.q, tid);
-            gf.fetch(gbase, a.d_o.sn, tile * kDiffTile, len.q, tid);
+            qf.fetch(tile * kDiffTile, len.q, tid);
+            gf.fetch(tile * kDiffTile, len.q, tid);
             if (tid < 128) {  // statistic tid / 32 of query tid % 32
                 const int qi = tile * kDiffTile + (tid & 31);
                 stat = tid < 64 ? INFINITY : 0.f;
@@ -240,7 +253,9 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_kernel(DiffArgs a) {
         fetch(tile_begin);
         store(0);
         lds_barrier();
-        for (int tile = tile_begin, at = 0; tile < tile_end; ++tile, at ^= 1) {
+        int tile = tile_begin;
+        auto step = [&](auto buffer) {
+            constexpr int at = decltype(buffer)::value;
             const bool more = tile + 1 < tile_end;
             if (more) fetch(tile + 1);
             if ((tile + 1) * kDiffTile > first_query) {  // (uniform in the wavefront)
@@ -290,6 +305,12 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_kernel(DiffArgs a) {
             }
             if (more) store(at ^ 1);
             lds_barrier();
+        };
+        while (tile < tile_end) {  // (one copy of the tile for each buffer)
+            step(std::integral_constant<int, 0>());
+            if (++tile >= tile_end) break;
+            step(std::integral_constant<int, 1>());
+            ++tile;
         }
     }
     if (key < a.n_k) {
