@@ -24,15 +24,18 @@ struct DiffArgs {
     const float *lq1, *lk1, *lq2, *lk2;
     float l_init;
     int l_step;                     // W / 2: a set of vectors for every head; 0: one set
-    float *lse;                     // saved: [2][B * heads * n_q], log2 of the softmax denominators; or null
+    float *ml;                      // saved: [4][B * heads * n_q], reference m of the first map (log2 units; +inf: sees no key), sum l of
+                                    // exp2(logit - m), then those of the second; or null
     void *o2;                       // saved: [B * heads * n_q][W], P2 V
     // forward pass over parts of the keys
     float *part;
     int splits, tiles_per_split;
     // gradient
     TensorArg d_o, dq, dk, dv;
-    float *rows_d;                  // [2][B * heads * n_q]: rowsum(dO o Om)
-    float *lam_part;                // [B * heads * row blocks]: sums of P2 o dP
+    float *stats;                   // [4][B * heads * n_q]: see diff_attn_rows_kernel
+    int parts;                      // of the tiles of a workgroup's rows or keys; each leaves sums of its own where there are several:
+    float *dq_part, *dkv_part;      // [parts][B * heads * n_q][W]; [parts][B * kv_heads * n_k][2 W]
+    float *lam_part;                // [B * heads * row blocks * parts]: sums of P2 o dP
     float *dlq1, *dlk1, *dlq2, *dlk2;
     int blocks;                     // blocks of rows (or keys) a (batch, head) has
     long long items;                // workgroups with work
@@ -185,6 +188,108 @@ struct DiffFetch {
     __device__ void store(unsigned char *tile, int tid) const {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) *(u32x4 *)(tile + Tile::off(i * kStep + tid / Tile::kChunks, tid % Tile::kChunks)) = x[i];
+    }
+};
+
+// bf16 tiles that loads bring straight into LDS, laid out as DiffTile (both kinds of reads), and read in assembly with waits of their
+// own: the compiler would wait for every load into LDS that is in flight in front of a read.  All offsets of a
+// lane's reads differ from its first one's by an exclusive or of small constants and by whole rows: one register holds them.
+typedef __attribute__((address_space(3))) void diff_lds_void;
+typedef const __attribute__((address_space(1))) void diff_global_cvoid;
+
+__device__ inline const char *diff_uniform(const void *ptr) {
+    const unsigned long long u = (unsigned long long)ptr;
+    const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)u), hi = __builtin_amdgcn_readfirstlane((unsigned)(u >> 32));
+    return (const char *)((unsigned long long)hi << 32 | lo);
+}
+__device__ inline void diff_landed(u32x4 (&x)[4]) {
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));
+}
+__device__ inline void diff_landed(u32x4 (&x)[2]) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1])); }
+__device__ inline void diff_landed(u32x4 (&x)[4], u32x4 (&y)[4]) {
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(y[0]), "+v"(y[1]), "+v"(y[2]), "+v"(y[3]));
+}
+__device__ inline void diff_landed(u32x4 (&x)[2], u32x4 (&y)[2]) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(y[0]), "+v"(y[1])); }
+__device__ inline void diff_landed(u32x4 (&x)[4], u32x4 (&y)[2]) {
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(y[0]), "+v"(y[1]));
+}
+__device__ inline void diff_landed(u32x4 (&x)[4], u32x4 (&y)[4], u32x4 (&z)[4]) {
+    asm volatile("s_waitcnt lgkmcnt(0)"
+                 : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(y[0]), "+v"(y[1]), "+v"(y[2]), "+v"(y[3]), "+v"(z[0]), "+v"(z[1]), "+v"(z[2]), "+v"(z[3]));
+}
+__device__ inline void diff_landed(u32x4 (&x)[4], u32x4 (&y)[2], u32x4 (&z)[2]) {
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(y[0]), "+v"(y[1]), "+v"(z[0]), "+v"(z[1]));
+}
+__device__ inline void diff_landed(u32x2 (&x)[8]) {
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]), "+v"(x[7]));
+}
+__device__ inline void diff_landed(u32x2 (&x)[4]) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3])); }
+__device__ inline f32x16 diff_join4(const u32x4 (&x)[4]) {
+    const f32x4 a = __builtin_bit_cast(f32x4, x[0]), b = __builtin_bit_cast(f32x4, x[1]), c = __builtin_bit_cast(f32x4, x[2]), d = __builtin_bit_cast(f32x4, x[3]);
+    return f32x16{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3], c[0], c[1], c[2], c[3], d[0], d[1], d[2], d[3]};
+}
+__device__ inline bf16x8 diff_join2(u32x2 a, u32x2 b) { return as_bf16x8(u32x4{a[0], a[1], b[0], b[1]}); }
+
+template <int W>
+struct DiffLds {
+    using Tile = DiffTile<__bf16, W>;
+    static constexpr int kRow = 2 * W, kKS = W / 32, kCB = W / 32;  // steps of 16 channels of a map, blocks of 32 channels
+    // The lane's first row-per-lane read of a tile at `tile`; operand ks is at that ^ 32 ks.
+    __device__ static unsigned rows(unsigned tile, int lane) { return tile + Tile::off(lane & 31, lane >> 5); }
+    // The lane's first transposing read; rows 8 further are at that ^ 32, + 8 rows; block cb at that ^ 64 cb.
+    __device__ static unsigned cols(unsigned tile, int lane) {
+        const int b = lane >> 4, j = lane & 15;
+        return tile + Tile::off(4 * (lane >> 5) + (j >> 2), (b & 1) * 2 + ((j & 3) >> 1)) + (j & 1) * 8;
+    }
+    template <int OFF>
+    __device__ static void read_rows(u32x4 (&x)[kKS], unsigned at, int from) {
+#pragma unroll
+        for (int ks = 0; ks < kKS; ++ks) x[ks] = lds_read_b128_at<OFF>(at ^ 32 * (from + ks));
+    }
+    // Operands of rows 16 KK .. + 15: piece 2 cb and 2 cb + 1 of block cb (join2).
+    template <int OFF, int KK>
+    __device__ static void read_cols(u32x2 (&x)[2 * kCB], unsigned at) {
+#pragma unroll
+        for (int cb = 0; cb < kCB; ++cb) {
+            x[2 * cb] = lds_read_tr16_at<OFF + 16 * KK * kRow>(at ^ 64 * cb);
+            x[2 * cb + 1] = lds_read_tr16_at<OFF + (16 * KK + 8) * kRow>(at ^ (64 * cb + 32));
+        }
+    }
+};
+
+// Loads of tiles into LDS by WAVES wavefronts, 1 KB an instruction: a lane fetches the chunk that belongs in its slot.  Rows at
+// `limit` and beyond are fetched as the one before it (the kernels mask them).
+template <int W, int WAVES>
+struct DiffDma {
+    using Tile = DiffTile<__bf16, W>;
+    static constexpr int kLoads = kDiffTile * W / (512 * WAVES), kRows = 512 / W, kChunks = W / 8;
+    const char *base;
+    long long step;
+    unsigned off[kLoads];
+    __device__ static unsigned chunk(int row, int slot) { return (Tile::off(row, slot) - row * 2 * W) / 16; }  // (its own inverse)
+    __device__ void start(const void *tensor, long long offset, long long sn, int wave, int lane) {
+        base = diff_uniform((const __bf16 *)tensor + offset);
+        step = 2 * sn;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) off[i] = (unsigned)(lane / kChunks) * (unsigned)step + 16 * chunk((wave * kLoads + i) * kRows + lane / kChunks, lane % kChunks);
+    }
+    __device__ void issue(unsigned char *tile, int row0, int limit, int wave, int lane) const {
+        const char *from = base + row0 * step;
+        if (row0 + kDiffTile <= limit) {  // (uniform)
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int first = (wave * kLoads + i) * kRows;
+                __builtin_amdgcn_global_load_lds((diff_global_cvoid *)(from + first * step + off[i]), (diff_lds_void *)(tile + first * 2 * W), 16, 0, 0);
+            }
+        } else {
+            asm("" : "+v"(lane));  // (worked out here: in registers all the way they would be missed)
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int first = (wave * kLoads + i) * kRows, row = first + lane / kChunks;
+                const unsigned at = (unsigned)min(row, limit - 1 - row0);
+                __builtin_amdgcn_global_load_lds((diff_global_cvoid *)(from + (at * (unsigned)step + 16 * chunk(row, lane % kChunks))), (diff_lds_void *)(tile + first * 2 * W), 16, 0, 0);
+            }
+        }
     }
 };
 

@@ -109,6 +109,15 @@ struct DiffPlace {
     }
 };
 
+// What the backward pass needs of a row: both references and sums.
+__device__ inline void diff_save(const DiffArgs &a, long long row, float m1, float l1, float m2, float l2) {
+    const long long n = diff_rows(a);
+    a.ml[row] = m1 == -INFINITY ? INFINITY : m1;
+    a.ml[n + row] = l1;
+    a.ml[2 * n + row] = m2 == -INFINITY ? INFINITY : m2;
+    a.ml[3 * n + row] = l2;
+}
+
 // Output of a wavefront's rows, or its part of it.
 template <typename T, typename TO, int W, bool SPLIT>
 __device__ inline void diff_finish(const DiffArgs &a, const DiffPlace &place, const DiffMap<W> &w1, const DiffMap<W> &w2, int lane) {
@@ -142,10 +151,7 @@ __device__ inline void diff_finish(const DiffArgs &a, const DiffPlace &place, co
     if (!place.row_live) return;
     const float inv1 = l1 > 0.f ? 1.f / l1 : l1, inv2 = l2 > 0.f ? 1.f / l2 : l2;  // (0 for a row that sees nothing, NaN stays NaN)
     const long long row = ((long long)place.b * a.heads + place.head) * a.n_q + place.qi;
-    if (a.lse && g == 0) {
-        a.lse[row] = w1.m == -INFINITY ? INFINITY : w1.m + log2f(l1);
-        a.lse[diff_rows(a) + row] = w2.m == -INFINITY ? INFINITY : w2.m + log2f(l2);
-    }
+    if (a.ml && g == 0) diff_save(a, row, w1.m, l1, w2.m, l2);
     TO *o = (TO *)const_cast<void *>(a.o.ptr) + place.b * a.o.sb + place.head * a.o.sh + place.qi * a.o.sn;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb)
@@ -289,29 +295,6 @@ __global__ void __launch_bounds__(64 * WAVES, 1) diff_attn_fwd_f32_kernel(DiffAr
 // Rows behind the last key are fetched as the last one, which is masked there.  Rows that see no key go along unmasked and are
 // dropped at the end.
 // ---------------------------------------------------------------------------------------
-typedef __attribute__((address_space(3))) void diff_lds_void;
-typedef const __attribute__((address_space(1))) void diff_global_cvoid;
-
-__device__ inline void diff_landed(u32x4 (&x)[4]) {
-    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));
-}
-__device__ inline void diff_landed(u32x4 (&x)[2]) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1])); }
-__device__ inline void diff_landed(u32x2 (&x)[8]) {
-    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]), "+v"(x[7]));
-}
-__device__ inline void diff_landed(u32x2 (&x)[4]) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3])); }
-
-// Layouts of a stage: K rows for row-per-lane reads, V rows for transposing ones (rows 8 apart are moved alike).
-template <int W>
-struct DiffStage {
-    static constexpr int kRow = 2 * W, kTile = kDiffTile * kRow, kBytes = 2 * kTile, kChunks = W / 8, kRing = 3;
-    __device__ static unsigned k_off(int row, int chunk) { return W == 128 ? wide_off_row(row, chunk) : tile_off_row(row, chunk); }
-    __device__ static unsigned v_off(int row, int chunk) { return W == 128 ? wide_off_tr(row, chunk) : tile_off_tr(row, chunk); }
-    // What 16-byte slot `slot` of a row holds (both layouts move chunks by exclusive or: its own inverse).
-    __device__ static unsigned k_chunk(int row, int slot) { return (k_off(row, slot) - row * kRow) / 16; }
-    __device__ static unsigned v_chunk(int row, int slot) { return (v_off(row, slot) - row * kRow) / 16; }
-};
-
 // Weights of a tile packed to bf16, and the running softmax: see diff_softmax.
 __device__ inline float diff_exp_pack(unsigned (&pk)[8], const f32x16 &s, float c, float minus_m) {
     float sum0 = 0.f, sum1 = 0.f;
@@ -342,11 +325,9 @@ __device__ inline void diff_softmax_pack(DiffMap<W> &w, unsigned (&pk)[8], const
 
 template <typename TO, int W, int WAVES, bool SPLIT>
 __global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffArgs a) {
-    using Stage = DiffStage<W>;
-    constexpr int KS = W / 32, CB = W / 32;           // steps of 16 channels of a map; blocks of 32 channels
-    constexpr int LOADS = kDiffTile * W / (512 * WAVES);  // instructions of 1 KB a wavefront and tile of K or V
-    constexpr int LOAD_ROWS = 512 / W;                // rows of one
-    __shared__ __align__(1024) unsigned char smem[Stage::kRing * Stage::kBytes];
+    using Lds = DiffLds<W>;
+    constexpr int KS = W / 32, CB = W / 32, TILE = kDiffTile * 2 * W, STAGE = 2 * TILE, RING = 3;  // a stage: K rows, then V rows
+    __shared__ __align__(1024) unsigned char smem[RING * STAGE];
     __shared__ int wave_most[WAVES];
     const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     DiffPlace place;
@@ -370,44 +351,12 @@ __global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffA
     int tile = SPLIT ? place.split * a.tiles_per_split : 0, tile_end = (most + kDiffTile - 1) / kDiffTile;
     if (SPLIT) tile_end = min(tile_end, tile + a.tiles_per_split);
 
-    // Loads of a tile: a wavefront's instructions cover LOAD_ROWS rows each; a lane fetches the chunk that belongs in its slot.
-    auto uniform = [](const void *ptr) {
-        const unsigned long long u = (unsigned long long)ptr;
-        const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)u), hi = __builtin_amdgcn_readfirstlane((unsigned)(u >> 32));
-        return (const char *)((unsigned long long)hi << 32 | lo);
-    };
-    const char *kbase = uniform((const __bf16 *)a.k.ptr + place.b * a.k.sb + place.kv * a.k.sh);
-    const char *vbase = uniform((const __bf16 *)a.v.ptr + place.b * a.v.sb + place.kv * a.v.sh);
-    const long long kstep = 2 * a.k.sn, vstep = 2 * a.v.sn;  // bytes from token to token
-    const int load_row = lane / Stage::kChunks, slot = lane % Stage::kChunks;
-    unsigned koff[LOADS], voff[LOADS];  // bytes from the tile's token of the instruction's first row
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-        const int row = (wave * LOADS + i) * LOAD_ROWS + load_row;
-        koff[i] = (unsigned)load_row * (unsigned)kstep + 16 * Stage::k_chunk(row, slot);
-        voff[i] = (unsigned)load_row * (unsigned)vstep + 16 * Stage::v_chunk(row, slot);
-    }
+    DiffDma<W, WAVES> kload, vload;
+    kload.start(a.k.ptr, place.b * a.k.sb + place.kv * a.k.sh, a.k.sn, wave, lane);
+    vload.start(a.v.ptr, place.b * a.v.sb + place.kv * a.v.sh, a.v.sn, wave, lane);
     auto issue = [&](int t, int to) {
-        unsigned char *kt = smem + to * Stage::kBytes, *vt = kt + Stage::kTile;
-        const char *kp = kbase + t * kDiffTile * kstep, *vp = vbase + t * kDiffTile * vstep;
-        if ((t + 1) * kDiffTile <= len.k) {  // (uniform)
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int row0 = (wave * LOADS + i) * LOAD_ROWS;
-                __builtin_amdgcn_global_load_lds((diff_global_cvoid *)(kp + row0 * kstep + koff[i]), (diff_lds_void *)(kt + row0 * Stage::kRow), 16, 0, 0);
-                __builtin_amdgcn_global_load_lds((diff_global_cvoid *)(vp + row0 * vstep + voff[i]), (diff_lds_void *)(vt + row0 * Stage::kRow), 16, 0, 0);
-            }
-        } else {
-            int l = lane;
-            asm("" : "+v"(l));  // (worked out here: in registers all the way they would be missed)
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int row0 = (wave * LOADS + i) * LOAD_ROWS, row = row0 + l / Stage::kChunks;
-                const unsigned from = (unsigned)min(row, len.k - 1 - t * kDiffTile);
-                __builtin_amdgcn_global_load_lds((diff_global_cvoid *)(kp + (from * (unsigned)kstep + 16 * Stage::k_chunk(row, l % Stage::kChunks))), (diff_lds_void *)(kt + row0 * Stage::kRow), 16, 0, 0);
-                __builtin_amdgcn_global_load_lds((diff_global_cvoid *)(vp + (from * (unsigned)vstep + 16 * Stage::v_chunk(row, l % Stage::kChunks))), (diff_lds_void *)(vt + row0 * Stage::kRow), 16, 0, 0);
-            }
-        }
+        kload.issue(smem + to * STAGE, t * kDiffTile, len.k, wave, lane);
+        vload.issue(smem + to * STAGE + TILE, t * kDiffTile, len.k, wave, lane);
     };
     DiffFrag<__bf16> q[2 * KS];
     {
@@ -427,33 +376,24 @@ __global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffA
         diff_zero(w1.acc[cb]);
         diff_zero(w2.acc[cb]);
     }
-    // Operand addresses of stage 0; a K operand's chunk 2 ks + g is exclusive-or'ed with 2 ks (formed at the read: one register).
-    unsigned kaddr = lds_address(smem) + Stage::k_off(li, g), vaddr[CB];
-    {
-        const int blk = lane >> 4, j = lane & 15;
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb)
-            vaddr[cb] = lds_address(smem) + Stage::kTile + Stage::v_off(4 * g + (j >> 2), cb * 4 + (blk & 1) * 2 + ((j & 3) >> 1)) + (j & 1) * 8;
-    }
+    const unsigned kaddr = Lds::rows(lds_address(smem), lane), vaddr = Lds::cols(lds_address(smem), lane);
     u32x4 k1[KS];
     if (tile < tile_end) {
 #pragma unroll
         for (int ks = 0; ks < 2 * KS; ++ks) asm volatile("" : "+v"(q[ks].x));  // (waited for here, not inside the loop)
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         lds_barrier();
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) k1[ks] = lds_read_b128_at<0>(kaddr ^ 32 * ks);
+        Lds::template read_rows<0>(k1, kaddr, 0);
         diff_landed(k1);
     }
     for (int stage = 0; tile < tile_end; ++tile) {
-        const int next = stage + 1 == Stage::kRing ? 0 : stage + 1, after = next + 1 == Stage::kRing ? 0 : next + 1;
-        const unsigned kat = kaddr + stage * Stage::kBytes, vat = stage * Stage::kBytes;
+        const int next = stage + 1 == RING ? 0 : stage + 1, after = next + 1 == RING ? 0 : next + 1;
+        const unsigned kat = kaddr + stage * STAGE, vat = vaddr + stage * STAGE;
         f32x16 s1, s2;
         diff_zero(s1);
         diff_zero(s2);
         u32x4 k2[KS];
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) k2[ks] = lds_read_b128_at<0>(kat ^ 32 * (KS + ks));
+        Lds::template read_rows<0>(k2, kat, KS);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) s1 = mfma32(as_bf16x8(k1[ks]), q[ks].x, s1);
@@ -478,11 +418,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffA
         unsigned p1[8], p2[8];
         diff_softmax_pack<W>(w1, p1, s1, a.c);
         u32x2 v0[2 * CB];
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-            v0[2 * cb] = lds_read_tr16_at<0>(vaddr[cb] + vat);
-            v0[2 * cb + 1] = lds_read_tr16_at<8 * Stage::kRow>(vaddr[cb] + vat);
-        }
+        Lds::template read_cols<TILE, 0>(v0, vat);
         __builtin_amdgcn_sched_barrier(0);
         diff_softmax_pack<W>(w2, p2, s2, a.c);
         auto products = [&](const u32x2 (&v)[2 * CB], int kk) {
@@ -490,24 +426,19 @@ __global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffA
             const bf16x8 b2 = as_bf16x8(u32x4{p2[4 * kk], p2[4 * kk + 1], p2[4 * kk + 2], p2[4 * kk + 3]});
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
-                const bf16x8 x = as_bf16x8(u32x4{v[2 * cb][0], v[2 * cb][1], v[2 * cb + 1][0], v[2 * cb + 1][1]});
+                const bf16x8 x = diff_join2(v[2 * cb], v[2 * cb + 1]);
                 w1.acc[cb] = mfma32(x, b1, w1.acc[cb]);
                 w2.acc[cb] = mfma32(x, b2, w2.acc[cb]);
             }
         };
         diff_landed(v0);
         u32x2 v1[2 * CB];
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-            v1[2 * cb] = lds_read_tr16_at<16 * Stage::kRow>(vaddr[cb] + vat);
-            v1[2 * cb + 1] = lds_read_tr16_at<24 * Stage::kRow>(vaddr[cb] + vat);
-        }
+        Lds::template read_cols<TILE, 1>(v1, vat);
         __builtin_amdgcn_sched_barrier(0);
         products(v0, 0);
         diff_landed(v1);
         // (after the last tile: of a stage that nobody needs)
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) k1[ks] = lds_read_b128_at<0>((kaddr + next * Stage::kBytes) ^ 32 * ks);
+        Lds::template read_rows<0>(k1, kaddr + next * STAGE, 0);
         __builtin_amdgcn_sched_barrier(0);
         products(v1, 1);
         diff_landed(k1);
@@ -562,10 +493,7 @@ __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
     const float lam = diff_lambda<W>(a, head, lane).value;
     const float inv1 = l1 > 0.f ? 1.f / l1 : l1, inv2 = l2 > 0.f ? 1.f / l2 : l2;
     const long long row = ((long long)b * a.heads + head) * a.n_q + qi;
-    if (a.lse && lane == 0) {
-        a.lse[row] = m1 == -INFINITY ? INFINITY : m1 + log2f(l1);
-        a.lse[diff_rows(a) + row] = m2 == -INFINITY ? INFINITY : m2 + log2f(l2);
-    }
+    if (a.ml && lane == 0) diff_save(a, row, m1, l1, m2, l2);
     TO *o = (TO *)const_cast<void *>(a.o.ptr) + b * a.o.sb + head * a.o.sh + qi * a.o.sn + lane * PER;
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
@@ -660,12 +588,12 @@ static DiffPlan diff_plan_of(const jv_diff_attn_desc *d) {
 
 size_t diff_saved_bytes(const jv_diff_attn_desc *d) {
     const size_t rows = (size_t)d->batch * d->heads * d->n_q;
-    return ((rows * 8 + 255) & ~(size_t)255) + rows * d->head_dim * (d->dtype == JV_BF16 ? 2 : 4);
+    return ((rows * 16 + 255) & ~(size_t)255) + rows * d->head_dim * (d->dtype == JV_BF16 ? 2 : 4);
 }
 void diff_use_saved(DiffProblem *p, void *saved) {
     const size_t rows = (size_t)diff_rows(p->a);
-    p->a.lse = (float *)saved;
-    p->a.o2 = (char *)saved + ((rows * 8 + 255) & ~(size_t)255);
+    p->a.ml = (float *)saved;
+    p->a.o2 = (char *)saved + ((rows * 16 + 255) & ~(size_t)255);
 }
 
 jv_status diff_problem(const jv_diff_attn_desc *d, const void *q, const void *k, const void *v, void *o,
@@ -679,7 +607,7 @@ jv_status diff_problem(const jv_diff_attn_desc *d, const void *q, const void *k,
     if (((uintptr_t)lambda->q1 | (uintptr_t)lambda->k1 | (uintptr_t)lambda->q2 | (uintptr_t)lambda->k2) & 3)
         return fail(JV_ERR_INVALID_ARG, "lambda's vectors must be 4-byte aligned");
     if (!(fabsf(lambda->init) <= 3.4028235e38f)) return fail(JV_ERR_INVALID_ARG, "lambda's init must be finite");
-    if (scale > 3.4028235e38f) return fail(JV_ERR_INVALID_ARG, "scale must be finite");
+    if (scale > 1e30f || (scale > 0.f && scale < 1e-30f)) return fail(JV_ERR_INVALID_ARG, "a scale of its own must lie between 1e-30 and 1e30");
     *p = DiffProblem{};
     DiffArgs &a = p->a;
     a.B = d->batch;

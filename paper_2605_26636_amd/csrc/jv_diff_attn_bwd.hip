@@ -9,7 +9,10 @@
 
 namespace jv {
 
-// D1, D2: row sums of dO o (P1 V) and dO o (P2 V), P1 V = O + lambda P2 V from the rounded rows that the forward pass left.
+// What both passes need of a query, from the rows of O and P2 V that the forward pass left in the element type
+// (P1 V = O + lambda P2 V) and its references and sums: a.stats holds
+//     [0], [1]   -log2(denominator of map m) / c, which a score product starts from: the weight is 2^(c sum), 0 for a row that sees no key
+//     [2]        -D1            [3]   -lambda (D1 - D2),    Dm = rowsum(dO o (Pm V)).
 // A row takes as many lanes as it has 16-byte pieces.
 template <typename T, int W>
 __global__ void __launch_bounds__(256) diff_attn_rows_kernel(DiffArgs a) {
@@ -52,114 +55,193 @@ __global__ void __launch_bounds__(256) diff_attn_rows_kernel(DiffArgs a) {
         d1 += __shfl_xor(d1, x);
         d2 += __shfl_xor(d2, x);
     }
-    if (live && ch == 0) {
-        a.rows_d[row] = d1;
-        a.rows_d[diff_rows(a) + row] = d2;
+    if (!live || ch) return;
+    const long long n = diff_rows(a);
+    const bool there = qi < DiffLengths(a, b).q;
+    for (int m = 0; m < 2; ++m) {
+        const float ref = there ? a.ml[2 * m * n + row] : INFINITY;
+        a.stats[m * n + row] = ref == INFINITY ? -INFINITY : -(ref + log2f(a.ml[(2 * m + 1) * n + row])) / a.c;
+    }
+    a.stats[2 * n + row] = -d1;
+    a.stats[3 * n + row] = -lam * (d1 - d2);
+}
+
+// One of a.parts equal parts of `total`: [from, to).
+__device__ inline void diff_part(const DiffArgs &a, int part, int total, int *from, int *to) {
+    *from = (int)((long long)total * part / a.parts);
+    *to = (int)((long long)total * (part + 1) / a.parts);
+}
+
+// What the query pass knows of a query: its weights are e inv with e = 2^(c score - m), and the gradients of its logits
+// dS1 = e1 (dP f1 + h1), dS2 = e2 (dP f2 + h2).
+struct DiffRowGrad {
+    float minus_m1, minus_m2, f1, h1, f2, h2, inv2;
+    __device__ void load(const DiffArgs &a, long long row, bool sees, float lam) {
+        minus_m1 = minus_m2 = -INFINITY;
+        f1 = h1 = f2 = h2 = inv2 = 0.f;
+        if (!sees) return;
+        const long long n = diff_rows(a);
+        minus_m1 = -a.ml[row];
+        minus_m2 = -a.ml[2 * n + row];
+        f1 = 1.f / a.ml[n + row];
+        inv2 = 1.f / a.ml[3 * n + row];
+        const float minus_d1 = a.stats[2 * n + row], lam_d2 = a.stats[3 * n + row] - lam * minus_d1;
+        h1 = minus_d1 * f1;
+        f2 = -lam * inv2;
+        h2 = lam_d2 * inv2;
+    }
+};
+
+// dQ of a wavefront's queries, or its part of it, and the workgroup's sum of P2 o dP.
+template <typename T, int W>
+__device__ inline void diff_finish_dq(const DiffArgs &a, const f32x16 (&acc)[W / 32], float lam_sum, int b, int h, int block, int part, float (&wave_lam)[4], int tid) {
+    const int lane = tid & 63, g = lane >> 5, wave = tid >> 6, qi = (block * 4 + wave) * 32 + (lane & 31);
+    const long long bh = (long long)b * a.heads + h;
+    if (qi < a.n_q) {
+        float *partial = a.dq_part + ((long long)part * diff_rows(a) + bh * a.n_q + qi) * W;
+        T *dq = (T *)const_cast<void *>(a.dq.ptr) + b * a.dq.sb + h * a.dq.sh + qi * a.dq.sn;
+#pragma unroll
+        for (int cb = 0; cb < W / 32; ++cb)
+#pragma unroll
+            for (int q4 = 0; q4 < 4; ++q4) {
+                const f32x16 &x = acc[cb];
+                const f32x4 y = {x[4 * q4] * a.scale, x[4 * q4 + 1] * a.scale, x[4 * q4 + 2] * a.scale, x[4 * q4 + 3] * a.scale};
+                const int ch = 32 * cb + 8 * q4 + 4 * g;
+                if (a.parts > 1) diff_store4(partial + ch, y);
+                else diff_store4(dq + ch, y);
+            }
+    }
+    lam_sum = wave_sum(lam_sum);
+    if (lane == 0) wave_lam[wave] = lam_sum;
+    __syncthreads();
+    if (tid == 0) a.lam_part[(bh * a.blocks + block) * a.parts + part] = (wave_lam[0] + wave_lam[1]) + (wave_lam[2] + wave_lam[3]);
+}
+
+// Where a workgroup of the query pass stands: 128 queries of a head, a part of the keys.
+struct DiffQueries {
+    int part, block, b, h, kv, qi, limit, most, least, tile, tile_end;
+    long long row;
+    bool row_live;
+    __device__ bool find(const DiffArgs &a, int (&wave_most)[4], int wave, int lane) {
+        long long item = diff_item(a.items);
+        if (item >= a.items) return false;
+        part = (int)(item % a.parts);
+        item /= a.parts;
+        block = a.blocks - 1 - (int)(item % a.blocks);  // causal: the longest rows first
+        const int bh = (int)(item / a.blocks);
+        b = bh / a.heads;
+        h = bh % a.heads;
+        kv = h / a.group;
+        qi = (block * 4 + wave) * 32 + (lane & 31);
+        row_live = qi < a.n_q;
+        row = (long long)bh * a.n_q + qi;
+        const DiffLengths len(a, b);
+        limit = row_live ? len.limit(a, qi) : 0;
+        most = limit;
+        least = limit > 0 ? limit : a.n_k + kDiffTile;  // (rows without a key have weights of zero without a mask)
+#pragma unroll
+        for (int x = 1; x < 32; x *= 2) {
+            most = max(most, __shfl_xor(most, x));
+            least = min(least, __shfl_xor(least, x));
+        }
+        if (lane == 0) wave_most[wave] = most;
+        __syncthreads();
+        most = __builtin_amdgcn_readfirstlane(max(max(wave_most[0], wave_most[1]), max(wave_most[2], wave_most[3])));
+        least = __builtin_amdgcn_readfirstlane(least);
+        diff_part(a, part, (most + kDiffTile - 1) / kDiffTile, &tile, &tile_end);
+        return true;
+    }
+};
+
+// Keys that a query does not see weigh nothing.
+__device__ inline void diff_hide_keys(f32x16 &s1, f32x16 &s2, int first, int limit, int g) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        const bool hidden = first + 8 * (v / 4) + 4 * g + v % 4 >= limit;
+        s1[v] = hidden ? -INFINITY : s1[v];
+        s2[v] = hidden ? -INFINITY : s2[v];
+    }
+}
+// Scores and dP of a tile (rows: keys) become the gradients of the logits, in place.
+__device__ inline void diff_logit_grads(f32x16 &s1, f32x16 &s2, const f32x16 &dp, const DiffRowGrad &r, float c, float &lam_sum) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        const float e1 = __builtin_amdgcn_exp2f(fmaf(s1[v], c, r.minus_m1)), e2 = __builtin_amdgcn_exp2f(fmaf(s2[v], c, r.minus_m2));
+        lam_sum = fmaf(e2, dp[v], lam_sum);
+        s1[v] = e1 * fmaf(dp[v], r.f1, r.h1);
+        s2[v] = e2 * fmaf(dp[v], r.f2, r.h2);
     }
 }
 
 // dQ, and the sums of P2 o dP (for lambda): a wavefront keeps 32 queries of one head, their dO and their dQ, and walks the keys.
 // A tile takes W / 16 score products, as many of V with dO, and as many of K^T with the gradients of the logits.
-template <typename T, int W>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) diff_attn_dq_kernel(DiffArgs a) {
+template <int W>
+__global__ void __launch_bounds__(256, 1) diff_attn_dq_f32_kernel(DiffArgs a) {
+    using T = float;
     using Tile = DiffTile<T, W>;
     constexpr int KS = W / 16, CB = W / 32;
     __shared__ __align__(16) unsigned char smem[2][2][Tile::kBytes];
     __shared__ int wave_most[4];
     __shared__ float wave_lam[4];
     const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const long long item = diff_item(a.items);
-    if (item >= a.items) return;  // whole workgroup
-    const int block = a.blocks - 1 - (int)(item % a.blocks), bh = (int)(item / a.blocks), b = bh / a.heads, h = bh % a.heads, kv = h / a.group;
-    const DiffLengths len(a, b);
-    const int qi = (block * 4 + wave) * 32 + li;
-    const bool row_live = qi < a.n_q;
-    const int limit = row_live ? len.limit(a, qi) : 0;
-    int most = limit, least = row_live ? limit : a.n_k;
-#pragma unroll
-    for (int x = 1; x < 32; x *= 2) {
-        most = max(most, __shfl_xor(most, x));
-        least = min(least, __shfl_xor(least, x));
-    }
-    if (lane == 0) wave_most[wave] = most;
-    __syncthreads();
-    most = __builtin_amdgcn_readfirstlane(most);
-    least = __builtin_amdgcn_readfirstlane(least);
-    const int wg_most = __builtin_amdgcn_readfirstlane(max(max(wave_most[0], wave_most[1]), max(wave_most[2], wave_most[3])));
-    const int tile_end = (wg_most + kDiffTile - 1) / kDiffTile;
-    const float lam = diff_lambda<W>(a, h, lane).value;
-
+    DiffQueries p;
+    if (!p.find(a, wave_most, wave, lane)) return;  // whole workgroup
+    const int len_k = DiffLengths(a, p.b).k;
+    const float lam = diff_lambda<W>(a, p.h, lane).value;
     DiffFrag<T> q[KS], go[KS];
-    const int q_at = row_live ? qi : 0;
+    DiffRowGrad r;
     {
-        const T *row = (const T *)a.q.ptr + b * a.q.sb + h * a.q.sh + q_at * a.q.sn, *grow = (const T *)a.d_o.ptr + b * a.d_o.sb + h * a.d_o.sh + q_at * a.d_o.sn;
+        const int at = p.row_live ? p.qi : 0;
+        const T *row = (const T *)a.q.ptr + p.b * a.q.sb + p.h * a.q.sh + at * a.q.sn, *grow = (const T *)a.d_o.ptr + p.b * a.d_o.sb + p.h * a.d_o.sh + at * a.d_o.sn;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            q[ks] = diff_global_frag<T>(row, ks, g, limit > 0);
-            go[ks] = diff_global_frag<T>(grow, ks, g, limit > 0);
+            q[ks] = diff_global_frag<T>(row, ks, g, p.limit > 0);
+            go[ks] = diff_global_frag<T>(grow, ks, g, p.limit > 0);
         }
+        r.load(a, p.row, p.limit > 0, lam);
     }
-    const long long at_row = (long long)bh * a.n_q + q_at;
-    const float lse1 = limit > 0 ? a.lse[at_row] : INFINITY, lse2 = limit > 0 ? a.lse[diff_rows(a) + at_row] : INFINITY;
-    const float d1 = limit > 0 ? a.rows_d[at_row] : 0.f, d2 = limit > 0 ? a.rows_d[diff_rows(a) + at_row] : 0.f;
     f32x16 acc[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) diff_zero(acc[cb]);
     float lam_sum = 0.f;
-
     DiffFetch<T, W, 256> kf, vf;
-    kf.start(a.k.ptr, b * a.k.sb + kv * a.k.sh, a.k.sn, tid);
-    vf.start(a.v.ptr, b * a.v.sb + kv * a.v.sh, a.v.sn, tid);
-    if (tile_end > 0) {
-        kf.fetch(0, len.k, tid);
-        vf.fetch(0, len.k, tid);
+    kf.start(a.k.ptr, p.b * a.k.sb + p.kv * a.k.sh, a.k.sn, tid);
+    vf.start(a.v.ptr, p.b * a.v.sb + p.kv * a.v.sh, a.v.sn, tid);
+    int tile = p.tile;
+    if (tile < p.tile_end) {
+        kf.fetch(tile * kDiffTile, len_k, tid);
+        vf.fetch(tile * kDiffTile, len_k, tid);
         kf.store(smem[0][0], tid);
         vf.store(smem[0][1], tid);
     }
     lds_barrier();
-    int tile = 0;
     auto step = [&](auto buffer) {
         constexpr int at = decltype(buffer)::value;
-        const bool more = tile + 1 < tile_end;
+        const bool more = tile + 1 < p.tile_end;
         if (more) {
-            kf.fetch((tile + 1) * kDiffTile, len.k, tid);
-            vf.fetch((tile + 1) * kDiffTile, len.k, tid);
+            kf.fetch((tile + 1) * kDiffTile, len_k, tid);
+            vf.fetch((tile + 1) * kDiffTile, len_k, tid);
         }
-        if (tile * kDiffTile < most) {  // (uniform in the wavefront)
-            const unsigned char *kt = smem[at][0], *vt = smem[at][1];
-            f32x16 s1, s2, dp;
-            diff_zero(s1);
-            diff_zero(s2);
-            diff_zero(dp);
+        const unsigned char *kt = smem[at][0], *vt = smem[at][1];
+        f32x16 s1, s2, dp;
+        diff_zero(s1);
+        diff_zero(s2);
+        diff_zero(dp);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const DiffFrag<T> k = Tile::row_frag(kt, li, ks, g);
-                if (ks < KS / 2) s1 = diff_mma(k, q[ks], s1);
-                else s2 = diff_mma(k, q[ks], s2);
-            }
+        for (int ks = 0; ks < KS; ++ks) {
+            const DiffFrag<T> k = Tile::row_frag(kt, li, ks, g);
+            if (ks < KS / 2) s1 = diff_mma(k, q[ks], s1);
+            else s2 = diff_mma(k, q[ks], s2);
+        }
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) dp = diff_mma(Tile::row_frag(vt, li, ks, g), go[ks], dp);
-            if ((tile + 1) * kDiffTile > least) {
+        for (int ks = 0; ks < KS; ++ks) dp = diff_mma(Tile::row_frag(vt, li, ks, g), go[ks], dp);
+        if ((tile + 1) * kDiffTile > p.least) diff_hide_keys(s1, s2, tile * kDiffTile, p.limit, g);
+        diff_logit_grads(s1, s2, dp, r, a.c, lam_sum);
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const bool hidden = tile * kDiffTile + 8 * (v / 4) + 4 * g + v % 4 >= limit;
-                    s1[v] = hidden ? -INFINITY : s1[v];
-                    s2[v] = hidden ? -INFINITY : s2[v];
-                }
-            }
+        for (int kk = 0; kk < 2; ++kk) {
+            const DiffFrag<T> ds1 = diff_block_frag<T>(s1, kk), ds2 = diff_block_frag<T>(s2, kk);
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const float p1 = __builtin_amdgcn_exp2f(fmaf(s1[v], a.c, -lse1)), p2 = __builtin_amdgcn_exp2f(fmaf(s2[v], a.c, -lse2));
-                lam_sum = fmaf(p2, dp[v], lam_sum);
-                s1[v] = p1 * (dp[v] - d1);
-                s2[v] = p2 * (dp[v] - d2) * -lam;
-            }
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-                const DiffFrag<T> ds1 = diff_block_frag<T>(s1, kk), ds2 = diff_block_frag<T>(s2, kk);
-#pragma unroll
-                for (int cb = 0; cb < CB; ++cb) acc[cb] = diff_mma(Tile::col_frag(kt, kk, cb, lane), cb < CB / 2 ? ds1 : ds2, acc[cb]);
-            }
+            for (int cb = 0; cb < CB; ++cb) acc[cb] = diff_mma(Tile::col_frag(kt, kk, cb, lane), cb < CB / 2 ? ds1 : ds2, acc[cb]);
         }
         if (more) {
             kf.store(smem[at ^ 1][0], tid);
@@ -167,54 +249,213 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) diff_attn_dq_kern
         }
         lds_barrier();
     };
-    while (tile < tile_end) {  // (one copy of the tile for each buffer)
+    while (tile < p.tile_end) {  // (one copy of the tile for each buffer, whose place is then part of the instructions)
         step(std::integral_constant<int, 0>());
-        if (++tile >= tile_end) break;
+        if (++tile >= p.tile_end) break;
         step(std::integral_constant<int, 1>());
         ++tile;
     }
-    if (row_live) {
-        T *dq = (T *)const_cast<void *>(a.dq.ptr) + b * a.dq.sb + h * a.dq.sh + qi * a.dq.sn;
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4) {
-                const f32x16 &x = acc[cb];
-                diff_store4(dq + 32 * cb + 8 * q4 + 4 * g,
-                            f32x4{x[4 * q4] * a.scale, x[4 * q4 + 1] * a.scale, x[4 * q4 + 2] * a.scale, x[4 * q4 + 3] * a.scale});
-            }
-    }
-    lam_sum = wave_sum(lam_sum);
-    if (lane == 0) wave_lam[wave] = lam_sum;
-    __syncthreads();
-    if (tid == 0) a.lam_part[(long long)bh * a.blocks + block] = (wave_lam[0] + wave_lam[1]) + (wave_lam[2] + wave_lam[3]);
+    diff_finish_dq<T, W>(a, acc, lam_sum * r.inv2, p.b, p.h, p.block, p.part, wave_lam, tid);
 }
 
-// dK and dV: a wavefront keeps 32 keys of one kv head, their values and both gradients, and walks the queries of the group's heads.
-// Lengths mask nothing here but the rows written: a query behind the end of its sequence has weights of zero (its
-// denominator is saved as infinite), and the columns of keys behind theirs are thrown away.
+// The same for bf16 tensors: tiles straight into two LDS stages, the next tile's under this one's arithmetic.
+template <int W>
+__global__ void __launch_bounds__(256, 2) diff_attn_dq_bf16_kernel(DiffArgs a) {
+    using Lds = DiffLds<W>;
+    constexpr int KS = W / 32, CB = W / 32, TILE = kDiffTile * 2 * W, STAGE = 2 * TILE;  // a stage: K rows, then V rows
+    __shared__ __align__(1024) unsigned char smem[2 * STAGE];
+    __shared__ int wave_most[4];
+    __shared__ float wave_lam[4];
+    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    DiffQueries p;
+    if (!p.find(a, wave_most, wave, lane)) return;  // whole workgroup
+    const int len_k = DiffLengths(a, p.b).k;
+    DiffDma<W, 4> kload, vload;
+    kload.start(a.k.ptr, p.b * a.k.sb + p.kv * a.k.sh, a.k.sn, wave, lane);
+    vload.start(a.v.ptr, p.b * a.v.sb + p.kv * a.v.sh, a.v.sn, wave, lane);
+    auto issue = [&](int t, int stage) {
+        kload.issue(smem + stage * STAGE, t * kDiffTile, len_k, wave, lane);
+        vload.issue(smem + stage * STAGE + TILE, t * kDiffTile, len_k, wave, lane);
+    };
+    int tile = p.tile;
+    if (tile < p.tile_end) issue(tile, 0);
+    const float lam = diff_lambda<W>(a, p.h, lane).value;
+    DiffFrag<__bf16> q[2 * KS], go[2 * KS];
+    DiffRowGrad r;
+    {
+        const int at = p.row_live ? p.qi : 0;
+        const __bf16 *row = (const __bf16 *)a.q.ptr + p.b * a.q.sb + p.h * a.q.sh + at * a.q.sn;
+        const __bf16 *grow = (const __bf16 *)a.d_o.ptr + p.b * a.d_o.sb + p.h * a.d_o.sh + at * a.d_o.sn;
+#pragma unroll
+        for (int ks = 0; ks < 2 * KS; ++ks) {
+            q[ks] = diff_global_frag<__bf16>(row, ks, g, p.limit > 0);
+            go[ks] = diff_global_frag<__bf16>(grow, ks, g, p.limit > 0);
+        }
+        r.load(a, p.row, p.limit > 0, lam);
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2 * KS; ++ks) asm volatile("" : "+v"(q[ks].x), "+v"(go[ks].x));  // (waited for here, not inside the loop)
+    asm volatile("" : "+v"(r.minus_m1), "+v"(r.minus_m2), "+v"(r.f1), "+v"(r.h1), "+v"(r.f2), "+v"(r.h2), "+v"(r.inv2));
+    f32x16 acc[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) diff_zero(acc[cb]);
+    float lam_sum = 0.f;
+    const unsigned rows0 = Lds::rows(lds_address(smem), lane), cols0 = Lds::cols(lds_address(smem), lane);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    lds_barrier();
+    for (int stage = 0; tile < p.tile_end; ++tile, stage ^= 1) {
+        if (tile + 1 < p.tile_end) issue(tile + 1, stage ^ 1);
+        const unsigned rows = rows0 + stage * STAGE, cols = cols0 + stage * STAGE;
+        f32x16 s1, s2, dp;
+        diff_zero(s1);
+        diff_zero(s2);
+        diff_zero(dp);
+        u32x4 x[KS], y[KS];
+        Lds::template read_rows<0>(x, rows, 0);
+        diff_landed(x);
+        Lds::template read_rows<0>(y, rows, KS);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s1 = mfma32(as_bf16x8(x[ks]), q[ks].x, s1);
+        diff_landed(y);
+        Lds::template read_rows<TILE>(x, rows, 0);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s2 = mfma32(as_bf16x8(y[ks]), q[KS + ks].x, s2);
+        diff_landed(x);
+        Lds::template read_rows<TILE>(y, rows, KS);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) dp = mfma32(as_bf16x8(x[ks]), go[ks].x, dp);
+        diff_landed(y);
+        u32x2 c0[2 * CB];
+        Lds::template read_cols<0, 0>(c0, cols);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) dp = mfma32(as_bf16x8(y[ks]), go[KS + ks].x, dp);
+        if ((tile + 1) * kDiffTile > p.least) diff_hide_keys(s1, s2, tile * kDiffTile, p.limit > 0 ? p.limit : a.n_k + kDiffTile, g);
+        diff_logit_grads(s1, s2, dp, r, a.c, lam_sum);
+        bf16x8 ds1[2], ds2[2];
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            ds1[kk] = diff_block_frag<__bf16>(s1, kk).x;
+            ds2[kk] = diff_block_frag<__bf16>(s2, kk).x;
+        }
+        diff_landed(c0);
+        u32x2 c1[2 * CB];
+        Lds::template read_cols<0, 1>(c1, cols);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) acc[cb] = mfma32(diff_join2(c0[2 * cb], c0[2 * cb + 1]), cb < CB / 2 ? ds1[0] : ds2[0], acc[cb]);
+        diff_landed(c1);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) acc[cb] = mfma32(diff_join2(c1[2 * cb], c1[2 * cb + 1]), cb < CB / 2 ? ds1[1] : ds2[1], acc[cb]);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the next tile, for every wavefront, and every wavefront done with this one
+        lds_barrier();
+    }
+    asm("" : "+v"(lam_sum));
+    diff_finish_dq<__bf16, W>(a, acc, lam_sum * r.inv2, p.b, p.h, p.block, p.part, wave_lam, tid);
+}
+
+// Where a workgroup of the key pass stands: 128 keys of a kv head; the tiles of its group's heads, one head after the other, of
+// which it takes a part.
+struct DiffKeys {
+    int part, block, b, kv, key, shift, first_query, tile_begin, n_tiles, from, to, len_q, len_k;
+    __device__ bool find(const DiffArgs &a, int wave, int lane) {
+        long long item = diff_item(a.items);
+        if (item >= a.items) return false;
+        part = (int)(item % a.parts);
+        item /= a.parts;
+        block = (int)(item % a.blocks);  // causal: the keys that most queries see first
+        const int bkv = (int)(item / a.blocks);
+        b = bkv / a.kv_heads;
+        kv = bkv % a.kv_heads;
+        const DiffLengths len(a, b);
+        len_q = len.q;
+        len_k = len.k;
+        const int key0 = block * 128;
+        key = key0 + wave * 32 + (lane & 31);
+        // causal: the first query that sees key x is x - (keys - queries)
+        shift = a.causal ? len_k - len_q : 0;
+        first_query = a.causal ? key0 + wave * 32 - shift : 0;
+        tile_begin = a.causal ? max(key0 - shift, 0) / kDiffTile : 0;
+        n_tiles = key0 < len_k ? max((len_q + kDiffTile - 1) / kDiffTile - tile_begin, 0) : 0;
+        diff_part(a, part, n_tiles * a.group, &from, &to);
+        return true;
+    }
+    // Masks of a tile whose rows are queries: those behind the last one, and, causal, those that do not see the lane's key.
+    __device__ bool masked(const DiffArgs &a, int tile) const { return (tile + 1) * kDiffTile > len_q || (a.causal && tile * kDiffTile < first_query + 31); }
+    __device__ void hide(const DiffArgs &a, f32x16 &s1, f32x16 &s2, int tile, int g) const {
+        const int from_query = a.causal ? key - shift : 0;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+            const int qi = tile * kDiffTile + 8 * (x / 4) + 4 * g + x % 4;
+            const bool hidden = qi < from_query || qi >= len_q;
+            s1[x] = hidden ? -INFINITY : s1[x];
+            s2[x] = hidden ? -INFINITY : s2[x];
+        }
+    }
+};
+
+// dK and dV of a wavefront's keys, or its part of them: zeros behind the last key.
 template <typename T, int W>
-__global__ void __launch_bounds__(256, 1) diff_attn_dkv_kernel(DiffArgs a) {
+__device__ inline void diff_finish_dkv(const DiffArgs &a, const f32x16 (&dk)[W / 32], const f32x16 (&dv)[W / 32], const DiffKeys &p, int g) {
+    if (p.key >= a.n_k) return;
+    const bool live = p.key < p.len_k;
+    T *krow = (T *)const_cast<void *>(a.dk.ptr) + p.b * a.dk.sb + p.kv * a.dk.sh + p.key * a.dk.sn;
+    T *vrow = (T *)const_cast<void *>(a.dv.ptr) + p.b * a.dv.sb + p.kv * a.dv.sh + p.key * a.dv.sn;
+    float *partial = a.dkv_part + (((long long)p.part * a.B * a.kv_heads + p.b * a.kv_heads + p.kv) * a.n_k + p.key) * (2 * W);
+#pragma unroll
+    for (int cb = 0; cb < W / 32; ++cb)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+            const int ch = 32 * cb + 8 * q4 + 4 * g;
+            f32x4 x, y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[e] = live ? dk[cb][4 * q4 + e] * a.scale : 0.f;
+                y[e] = live ? dv[cb][4 * q4 + e] : 0.f;
+            }
+            if (a.parts > 1) {
+                diff_store4(partial + ch, x);
+                diff_store4(partial + W + ch, y);
+            } else {
+                diff_store4(krow + ch, x);
+                diff_store4(vrow + ch, y);
+            }
+        }
+}
+
+// Row x of a block: the score (which started from the stored logarithm) of both maps, dP - D1 and -lambda (D1 - D2) become the
+// gradients of the logits and P1 - lambda P2.
+__device__ inline void diff_weights_and_grads(f32x16 &s1, f32x16 &s2, f32x16 &dp, int x, float minus_lam_d, float c, float lam) {
+    const float p1 = __builtin_amdgcn_exp2f(s1[x] * c), p2 = __builtin_amdgcn_exp2f(s2[x] * c);
+    s1[x] = p1 * dp[x];
+    s2[x] = p2 * fmaf(-lam, dp[x], minus_lam_d);
+    dp[x] = fmaf(-lam, p2, p1);
+}
+
+// dK and dV: a wavefront keeps 32 keys of one kv head and both gradients, and walks the queries of the group's heads.  What
+// lengths hide is the columns of keys behind the last, which are thrown away, and the rows of queries behind the last.
+template <int W>
+__global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
+    using T = float;
     using Tile = DiffTile<T, W>;
     constexpr int KS = W / 16, CB = W / 32;
     __shared__ __align__(16) unsigned char smem[2][2][Tile::kBytes];
-    __shared__ __align__(16) float stats[2][4][kDiffTile];  // of a tile's queries: both denominators, D1, D2
+    __shared__ __align__(16) float stats[2][4][kDiffTile];
     const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const long long item = diff_item(a.items);
-    if (item >= a.items) return;  // whole workgroup
-    const int block = (int)(item % a.blocks), bkv = (int)(item / a.blocks), b = bkv / a.kv_heads, kv = bkv % a.kv_heads;
-    const DiffLengths len(a, b);
-    const int key0 = block * 128, key = key0 + wave * 32 + li;
-    const bool key_live = key < len.k;
-
+    DiffKeys p;
+    if (!p.find(a, wave, lane)) return;  // whole workgroup
     DiffFrag<T> k[KS], v[KS];
     {
-        const int at = key_live ? key : 0;
-        const T *krow = (const T *)a.k.ptr + b * a.k.sb + kv * a.k.sh + at * a.k.sn, *vrow = (const T *)a.v.ptr + b * a.v.sb + kv * a.v.sh + at * a.v.sn;
+        const bool live = p.key < p.len_k;
+        const int at = live ? p.key : 0;
+        const T *krow = (const T *)a.k.ptr + p.b * a.k.sb + p.kv * a.k.sh + at * a.k.sn, *vrow = (const T *)a.v.ptr + p.b * a.v.sb + p.kv * a.v.sh + at * a.v.sn;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-            k[ks] = diff_global_frag<T>(krow, ks, g, key_live);
-            v[ks] = diff_global_frag<T>(vrow, ks, g, key_live);
+            k[ks] = diff_global_frag<T>(krow, ks, g, live);
+            v[ks] = diff_global_frag<T>(vrow, ks, g, live);
         }
     }
     f32x16 dk[CB], dv[CB];
@@ -223,113 +464,262 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_kernel(DiffArgs a) {
         diff_zero(dk[cb]);
         diff_zero(dv[cb]);
     }
-    // causal: the first query that sees key x is x - (keys - queries)
-    const int shift = a.causal ? len.k - len.q : 0;
-    const int tile_begin = a.causal ? max(key0 - shift, 0) / kDiffTile : 0, tile_end = key0 < len.k ? (len.q + kDiffTile - 1) / kDiffTile : 0;
-    const int n_tiles = max(tile_end - tile_begin, 0);
-    const int first_query = a.causal ? key0 + wave * 32 - shift : 0;  // the wavefront's keys are seen from here on
-    for (int hg = 0; hg < (n_tiles ? a.group : 0); ++hg) {
-        const int h = kv * a.group + hg;
-        const float lam = diff_lambda<W>(a, h, lane).value;
-        const long long row0 = ((long long)b * a.heads + h) * a.n_q;
-        DiffFetch<T, W, 256> qf, gf;
-        qf.start(a.q.ptr, b * a.q.sb + h * a.q.sh, a.q.sn, tid);
-        gf.start(a.d_o.ptr, b * a.d_o.sb + h * a.d_o.sh, a.d_o.sn, tid);
-        float stat = 0.f;
-        auto fetch = [&](int tile) {
-            qf.fetch(tile * kDiffTile, len.q, tid);
-            gf.fetch(tile * kDiffTile, len.q, tid);
-            if (tid < 128) {  // statistic tid / 32 of query tid % 32
-                const int qi = tile * kDiffTile + (tid & 31);
-                stat = tid < 64 ? INFINITY : 0.f;
-                if (qi < len.q) stat = (tid < 64 ? a.lse : a.rows_d)[(tid >> 5 & 1 ? diff_rows(a) : 0) + row0 + qi];
-            }
-        };
-        auto store = [&](int to) {
-            qf.store(smem[to][0], tid);
-            gf.store(smem[to][1], tid);
-            if (tid < 128) stats[to][tid >> 5][tid & 31] = stat;
-        };
-        fetch(tile_begin);
+    DiffFetch<T, W, 256> qf, gf;
+    float stat = 0.f;
+    auto fetch = [&](int at) {
+        const int h = p.kv * a.group + at / p.n_tiles, row0 = (p.tile_begin + at % p.n_tiles) * kDiffTile;
+        qf.start(a.q.ptr, p.b * a.q.sb + h * a.q.sh, a.q.sn, tid);
+        gf.start(a.d_o.ptr, p.b * a.d_o.sb + h * a.d_o.sh, a.d_o.sn, tid);
+        qf.fetch(row0, p.len_q, tid);
+        gf.fetch(row0, p.len_q, tid);
+        if (tid < 128) stat = a.stats[(tid >> 5) * diff_rows(a) + ((long long)p.b * a.heads + h) * a.n_q + min(row0 + (tid & 31), a.n_q - 1)];
+    };
+    auto store = [&](int to) {
+        qf.store(smem[to][0], tid);
+        gf.store(smem[to][1], tid);
+        if (tid < 128) stats[to][tid >> 5][tid & 31] = stat;
+    };
+    if (p.from < p.to) {
+        fetch(p.from);
         store(0);
-        lds_barrier();
-        int tile = tile_begin;
-        auto step = [&](auto buffer) {
-            constexpr int at = decltype(buffer)::value;
-            const bool more = tile + 1 < tile_end;
-            if (more) fetch(tile + 1);
-            if ((tile + 1) * kDiffTile > first_query) {  // (uniform in the wavefront)
-                const unsigned char *qt = smem[at][0], *gt = smem[at][1];
-                f32x16 s1, s2, dp;
-                diff_zero(s1);
-                diff_zero(s2);
-                diff_zero(dp);
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    const DiffFrag<T> q = Tile::row_frag(qt, li, ks, g);
-                    if (ks < KS / 2) s1 = diff_mma(q, k[ks], s1);
-                    else s2 = diff_mma(q, k[ks], s2);
-                }
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) dp = diff_mma(Tile::row_frag(gt, li, ks, g), v[ks], dp);
-                if (a.causal && tile * kDiffTile < first_query + 31) {
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        const bool hidden = key > tile * kDiffTile + 8 * (x / 4) + 4 * g + x % 4 + shift;
-                        s1[x] = hidden ? -INFINITY : s1[x];
-                        s2[x] = hidden ? -INFINITY : s2[x];
-                    }
-                }
-#pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4) {
-                    const f32x4 lse1 = *(const f32x4 *)&stats[at][0][8 * q4 + 4 * g], lse2 = *(const f32x4 *)&stats[at][1][8 * q4 + 4 * g];
-                    const f32x4 d1 = *(const f32x4 *)&stats[at][2][8 * q4 + 4 * g], d2 = *(const f32x4 *)&stats[at][3][8 * q4 + 4 * g];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int x = 4 * q4 + e;
-                        const float p1 = __builtin_amdgcn_exp2f(fmaf(s1[x], a.c, -lse1[e])), p2 = -lam * __builtin_amdgcn_exp2f(fmaf(s2[x], a.c, -lse2[e]));
-                        s1[x] = p1 * (dp[x] - d1[e]);
-                        s2[x] = p2 * (dp[x] - d2[e]);
-                        dp[x] = p1 + p2;
-                    }
-                }
-#pragma unroll
-                for (int kk = 0; kk < 2; ++kk) {
-                    const DiffFrag<T> p = diff_block_frag<T>(dp, kk), ds1 = diff_block_frag<T>(s1, kk), ds2 = diff_block_frag<T>(s2, kk);
-#pragma unroll
-                    for (int cb = 0; cb < CB; ++cb) {
-                        dv[cb] = diff_mma(Tile::col_frag(gt, kk, cb, lane), p, dv[cb]);
-                        dk[cb] = diff_mma(Tile::col_frag(qt, kk, cb, lane), cb < CB / 2 ? ds1 : ds2, dk[cb]);
-                    }
-                }
-            }
-            if (more) store(at ^ 1);
-            lds_barrier();
-        };
-        while (tile < tile_end) {  // (one copy of the tile for each buffer)
-            step(std::integral_constant<int, 0>());
-            if (++tile >= tile_end) break;
-            step(std::integral_constant<int, 1>());
-            ++tile;
+    }
+    lds_barrier();
+    float lam = 0.f;
+    int head = -1;
+    for (int at = p.from, buffer = 0; at < p.to; ++at, buffer ^= 1) {
+        if (at / p.n_tiles != head) {  // (uniform)
+            head = at / p.n_tiles;
+            lam = diff_lambda<W>(a, p.kv * a.group + head, lane).value;
         }
-    }
-    if (key < a.n_k) {
-        T *krow = (T *)const_cast<void *>(a.dk.ptr) + b * a.dk.sb + kv * a.dk.sh + key * a.dk.sn;
-        T *vrow = (T *)const_cast<void *>(a.dv.ptr) + b * a.dv.sb + kv * a.dv.sh + key * a.dv.sn;
+        const bool more = at + 1 < p.to;
+        if (more) fetch(at + 1);
+        const int tile = p.tile_begin + at % p.n_tiles;
+        if ((tile + 1) * kDiffTile > p.first_query) {  // (uniform in the wavefront)
+            const unsigned char *qt = smem[buffer][0], *gt = smem[buffer][1];
+            f32x16 s1, s2, dp;
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-            for (int q4 = 0; q4 < 4; ++q4) {
-                f32x4 x, y;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[e] = key_live ? dk[cb][4 * q4 + e] * a.scale : 0.f;
-                    y[e] = key_live ? dv[cb][4 * q4 + e] : 0.f;
-                }
-                diff_store4(krow + 32 * cb + 8 * q4 + 4 * g, x);
-                diff_store4(vrow + 32 * cb + 8 * q4 + 4 * g, y);
+            for (int x = 0; x < 16; ++x) {
+                s1[x] = stats[buffer][0][8 * (x / 4) + 4 * g + x % 4];
+                s2[x] = stats[buffer][1][8 * (x / 4) + 4 * g + x % 4];
+                dp[x] = stats[buffer][2][8 * (x / 4) + 4 * g + x % 4];
             }
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const DiffFrag<T> q = Tile::row_frag(qt, li, ks, g);
+                if (ks < KS / 2) s1 = diff_mma(q, k[ks], s1);
+                else s2 = diff_mma(q, k[ks], s2);
+            }
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) dp = diff_mma(Tile::row_frag(gt, li, ks, g), v[ks], dp);
+            if (p.masked(a, tile)) p.hide(a, s1, s2, tile, g);
+#pragma unroll
+            for (int x = 0; x < 16; ++x) diff_weights_and_grads(s1, s2, dp, x, stats[buffer][3][8 * (x / 4) + 4 * g + x % 4], a.c, lam);
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+                const DiffFrag<T> w = diff_block_frag<T>(dp, kk), ds1 = diff_block_frag<T>(s1, kk), ds2 = diff_block_frag<T>(s2, kk);
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) {
+                    dv[cb] = diff_mma(Tile::col_frag(gt, kk, cb, lane), w, dv[cb]);
+                    dk[cb] = diff_mma(Tile::col_frag(qt, kk, cb, lane), cb < CB / 2 ? ds1 : ds2, dk[cb]);
+                }
+            }
+        }
+        if (more) store(buffer ^ 1);
+        lds_barrier();
     }
+    diff_finish_dkv<T, W>(a, dk, dv, p, g);
+}
+
+// The same for bf16 tensors.  K operands stay in registers, V in LDS (with both gradients, 4 W / 32 accumulators of 16 registers, there
+// is no room for it at two wavefronts a SIMD); tiles of Q and dO and the queries' statistics come straight into two LDS stages, the
+// next tile's under this one's arithmetic.  Score products start from the stored logarithms and dP from -D1, read from LDS into the
+// accumulators.  LDS gives 40 + 8 KB a tile and wavefront for 4 W / 16 matrix instructions.
+template <int W>
+__global__ void __launch_bounds__(256, 2) diff_attn_dkv_bf16_kernel(DiffArgs a) {
+    using Lds = DiffLds<W>;
+    constexpr int KS = W / 32, CB = W / 32, TILE = kDiffTile * 2 * W, STATS = 4 * kDiffTile * 4, STAGE = 2 * TILE + 1024;  // Q rows, dO rows, statistics
+    static_assert(STATS <= 1024, "stages stay 1 KB aligned");
+    __shared__ __align__(1024) unsigned char smem[2 * STAGE + 4 * TILE];
+    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    DiffKeys p;
+    if (!p.find(a, wave, lane)) return;  // whole workgroup
+    unsigned char *vt = smem + 2 * STAGE + wave * TILE;  // the wavefront's own values
+    DiffDma<W, 4> qload, gload;
+    int next_tile = p.tile_begin, next_head = p.kv * a.group;
+    if (p.n_tiles) {
+        next_head += p.from / p.n_tiles;
+        next_tile += p.from % p.n_tiles;
+    }
+    qload.start(a.q.ptr, p.b * a.q.sb + next_head * a.q.sh, a.q.sn, wave, lane);
+    gload.start(a.d_o.ptr, p.b * a.d_o.sb + next_head * a.d_o.sh, a.d_o.sn, wave, lane);
+    // Loads of the next tile into a stage, and on to the one after.
+    auto issue = [&](int stage) {
+        unsigned char *to = smem + stage * STAGE;
+        const int row0 = next_tile * kDiffTile;
+        qload.issue(to, row0, p.len_q, wave, lane);
+        gload.issue(to + TILE, row0, p.len_q, wave, lane);
+        if (wave < 2) {  // statistics 2 wave and 2 wave + 1
+            const char *from = diff_uniform(a.stats + 2 * wave * diff_rows(a) + ((long long)p.b * a.heads + next_head) * a.n_q + row0);
+            const long long other = diff_rows(a) * 4;
+            const unsigned at = 4 * min(lane & 31, p.len_q - 1 - row0);
+            __builtin_amdgcn_global_load_lds((diff_global_cvoid *)(from + (lane >> 5) * other + at), (diff_lds_void *)(to + 2 * TILE + wave * 256), 4, 0, 0);
+        }
+        if (++next_tile == p.tile_begin + p.n_tiles) {
+            next_tile = p.tile_begin;
+            ++next_head;
+            qload.base += 2 * a.q.sh;
+            gload.base += 2 * a.d_o.sh;
+        }
+    };
+    u32x4 k[2 * KS];
+    if (p.from < p.to) {
+        DiffDma<W, 1> vload;
+        const int key0 = p.block * 128 + wave * 32;
+        vload.start(a.v.ptr, p.b * a.v.sb + p.kv * a.v.sh, a.v.sn, 0, lane);
+        if (key0 < p.len_k) vload.issue(vt, key0, p.len_k, 0, lane);
+        const bool live = p.key < p.len_k;
+        const __bf16 *row = (const __bf16 *)a.k.ptr + p.b * a.k.sb + p.kv * a.k.sh + (live ? p.key : 0) * a.k.sn;
+#pragma unroll
+        for (int ks = 0; ks < 2 * KS; ++ks) k[ks] = as_u32x4(diff_global_frag<__bf16>(row, ks, g, live).x);
+#pragma unroll
+        for (int ks = 0; ks < 2 * KS; ++ks) asm volatile("" : "+v"(k[ks]));  // (waited for here, not inside the loop)
+        issue(0);
+    }
+    f32x16 dk[CB], dv[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+        diff_zero(dk[cb]);
+        diff_zero(dv[cb]);
+    }
+    const unsigned rows0 = Lds::rows(lds_address(smem), lane), cols0 = Lds::cols(lds_address(smem), lane), stats0 = lds_address(smem) + 2 * TILE + 16 * g;
+    const unsigned vrows = Lds::rows(lds_address(vt), lane);
+    float lam = 0.f;
+    int tile = 0, left = 0, head = 0;  // tiles left of the present head
+    if (p.n_tiles) {
+        head = p.kv * a.group + p.from / p.n_tiles;
+        tile = p.tile_begin + p.from % p.n_tiles;
+        left = p.n_tiles - p.from % p.n_tiles;
+        lam = diff_lambda<W>(a, head, lane).value;
+    }
+    lam = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, lam)));
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    lds_barrier();
+    for (int at = p.from, stage = 0; at < p.to; ++at, stage ^= 1) {
+        if (at + 1 < p.to) issue(stage ^ 1);
+        const unsigned rows = rows0 + stage * STAGE, cols = cols0 + stage * STAGE, stats = stats0 + stage * STAGE;
+        auto read_stats = [&](u32x4 (&to)[4], auto which) {
+            constexpr int at0 = decltype(which)::value * kDiffTile * 4;
+            to[0] = lds_read_b128_at<at0>(stats);
+            to[1] = lds_read_b128_at<at0 + 32>(stats);
+            to[2] = lds_read_b128_at<at0 + 64>(stats);
+            to[3] = lds_read_b128_at<at0 + 96>(stats);
+        };
+        f32x16 s1, s2, dp;
+        {
+            u32x4 i1[4], i2[4], x[KS], y[KS];
+            read_stats(i1, std::integral_constant<int, 0>());
+            Lds::template read_rows<0>(x, rows, 0);
+            diff_landed(i1, x);
+            read_stats(i2, std::integral_constant<int, 1>());
+            Lds::template read_rows<0>(y, rows, KS);
+            __builtin_amdgcn_sched_barrier(0);
+            s1 = diff_join4(i1);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) s1 = mfma32(as_bf16x8(x[ks]), as_bf16x8(k[ks]), s1);
+            diff_landed(i2, y);
+            s2 = diff_join4(i2);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) s2 = mfma32(as_bf16x8(y[ks]), as_bf16x8(k[KS + ks]), s2);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        {
+            u32x4 i3[4], x[2], v[2];
+            read_stats(i3, std::integral_constant<int, 2>());
+#pragma unroll
+            for (int ks = 0; ks < 2 * KS; ks += 2) {  // two operands of each at a time: more would not fit the registers
+                x[0] = lds_read_b128_at<TILE>(rows ^ 32 * ks);
+                x[1] = lds_read_b128_at<TILE>(rows ^ 32 * (ks + 1));
+                v[0] = lds_read_b128_at<0>(vrows ^ 32 * ks);
+                v[1] = lds_read_b128_at<0>(vrows ^ 32 * (ks + 1));
+                if (ks == 0) {
+                    diff_landed(i3, x, v);
+                    dp = diff_join4(i3);
+                } else {
+                    diff_landed(x, v);
+                }
+                dp = mfma32(as_bf16x8(x[0]), as_bf16x8(v[0]), dp);
+                dp = mfma32(as_bf16x8(x[1]), as_bf16x8(v[1]), dp);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        u32x4 init[4];
+        read_stats(init, std::integral_constant<int, 3>());
+        __builtin_amdgcn_sched_barrier(0);
+        if (p.masked(a, tile)) p.hide(a, s1, s2, tile, g);
+        diff_landed(init);
+        {
+            const f32x16 minus_lam_d = diff_join4(init);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) diff_weights_and_grads(s1, s2, dp, e, minus_lam_d[e], a.c, lam);
+        }
+        bf16x8 w[2], ds1[2], ds2[2];
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            w[kk] = diff_block_frag<__bf16>(dp, kk).x;
+            ds1[kk] = diff_block_frag<__bf16>(s1, kk).x;
+            ds2[kk] = diff_block_frag<__bf16>(s2, kk).x;
+        }
+        u32x2 c0[2 * CB], c1[2 * CB];
+        Lds::template read_cols<TILE, 0>(c0, cols);
+        diff_landed(c0);
+        Lds::template read_cols<TILE, 1>(c1, cols);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) dv[cb] = mfma32(diff_join2(c0[2 * cb], c0[2 * cb + 1]), w[0], dv[cb]);
+        diff_landed(c1);
+        Lds::template read_cols<0, 0>(c0, cols);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) dv[cb] = mfma32(diff_join2(c1[2 * cb], c1[2 * cb + 1]), w[1], dv[cb]);
+        diff_landed(c0);
+        Lds::template read_cols<0, 1>(c1, cols);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) dk[cb] = mfma32(diff_join2(c0[2 * cb], c0[2 * cb + 1]), cb < CB / 2 ? ds1[0] : ds2[0], dk[cb]);
+        diff_landed(c1);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb) dk[cb] = mfma32(diff_join2(c1[2 * cb], c1[2 * cb + 1]), cb < CB / 2 ? ds1[1] : ds2[1], dk[cb]);
+        ++tile;
+        if (--left == 0 && at + 1 < p.to) {  // on to the group's next head (uniform)
+            tile = p.tile_begin;
+            left = p.n_tiles;
+            lam = diff_lambda<W>(a, ++head, lane).value;
+            lam = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, lam)));
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the next tile, for every wavefront, and every wavefront done with this one
+        lds_barrier();
+    }
+    diff_finish_dkv<__bf16, W>(a, dk, dv, p, g);
+}
+
+// Parts of rows of `channels` fp32 numbers added in their order: row (x, h, n) of B x heads x n rows to tensor `out`, and its channels
+// from W on to `out2`.  Rows at the sequence's end (`len`, or null) and beyond hold zeros.
+template <typename T, int W>
+__global__ void __launch_bounds__(256) diff_attn_sum_kernel(const float *part, int parts, long long rows, int heads, int n, TensorArg out, TensorArg out2, int channels) {
+    const int per_row = channels / 4;
+    const long long at = (long long)blockIdx.x * 256 + threadIdx.x, row = at / per_row;
+    if (row >= rows) return;
+    const int ch = (int)(at % per_row) * 4;
+    f32x4 sum = *(const f32x4 *)(part + row * channels + ch);
+    for (int p = 1; p < parts; ++p) {
+        const f32x4 x = *(const f32x4 *)(part + (p * rows + row) * channels + ch);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += x[e];
+    }
+    const int i = (int)(row % n), bh = (int)(row / n), h = bh % heads, b = bh / heads;
+    const TensorArg &to = ch < W ? out : out2;
+    diff_store4((T *)const_cast<void *>(to.ptr) + b * to.sb + h * to.sh + i * to.sn + (ch < W ? ch : ch - W), sum);
 }
 
 // Gradients of lambda's vectors from the sums of P2 o dP: dlambda_h is their negative sum, over the heads too where these share
@@ -339,12 +729,13 @@ __global__ void __launch_bounds__(1024) diff_attn_dlambda_kernel(DiffArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     __shared__ double shared_sum[16];
     const int sets = a.l_step ? a.heads : 1;
-    const long long per_image = (long long)a.heads * a.blocks;
+    const int sums = a.blocks * a.parts;  // of a (batch, head)
+    const long long per_image = (long long)a.heads * sums;
     for (int set = a.l_step ? wave : 0; set < sets; set += a.l_step ? waves : 1) {
         double sum = 0.0;
         if (a.l_step) {
-            const long long n = (long long)a.B * a.blocks;
-            for (long long x = lane; x < n; x += 64) sum += a.lam_part[x / a.blocks * per_image + (long long)set * a.blocks + x % a.blocks];
+            const long long n = (long long)a.B * sums;
+            for (long long x = lane; x < n; x += 64) sum += a.lam_part[x / sums * per_image + (long long)set * sums + x % sums];
         } else {
             for (long long x = threadIdx.x; x < a.B * per_image; x += blockDim.x) sum += a.lam_part[x];
         }
@@ -370,29 +761,66 @@ __global__ void __launch_bounds__(1024) diff_attn_dlambda_kernel(DiffArgs a) {
     }
 }
 
+// Parts of the tiles that the workgroups of a pass are cut into: as many as bring `items` workgroups (of which a chip holds 512) to
+// 1 024, of eight tiles at least, 16 at most.
+static int diff_bwd_parts(long long items, long long tiles) {
+    const long long parts = items >= 512 ? 1 : (1024 + items - 1) / items;
+    return (int)std::max(1ll, std::min({parts, tiles / 8, 16ll}));
+}
+struct DiffBwdPlan {
+    int q_blocks, k_blocks, q_parts, k_parts;
+    size_t stats, lam, dq, dkv;  // bytes of the workspace's pieces, in this order
+};
+static DiffBwdPlan diff_bwd_plan(const jv_diff_attn_desc *d) {
+    DiffBwdPlan p;
+    p.q_blocks = (d->n_q + 127) / 128;
+    p.k_blocks = (d->n_k + 127) / 128;
+    const long long group = d->heads / d->kv_heads, rows = (long long)d->batch * d->heads * d->n_q, keys = (long long)d->batch * d->kv_heads * d->n_k;
+    p.q_parts = diff_bwd_parts((long long)d->batch * d->heads * p.q_blocks, (d->n_k + kDiffTile - 1) / kDiffTile);
+    p.k_parts = diff_bwd_parts((long long)d->batch * d->kv_heads * p.k_blocks, (d->n_q + kDiffTile - 1) / kDiffTile * group);
+    auto whole = [](long long bytes) { return ((size_t)bytes + 255) & ~(size_t)255; };
+    p.stats = whole(rows * 16);
+    p.lam = whole((long long)d->batch * d->heads * p.q_blocks * p.q_parts * 4);
+    p.dq = p.q_parts > 1 ? whole(rows * p.q_parts * d->head_dim * 4) : 0;
+    p.dkv = p.k_parts > 1 ? whole(keys * p.k_parts * d->head_dim * 8) : 0;
+    return p;
+}
+
 template <typename T, int W>
-static jv_status diff_backward(DiffArgs a, hipStream_t stream) {
-    const long long rows = diff_rows(a);
+static jv_status diff_backward(DiffArgs a, const DiffBwdPlan &plan, hipStream_t stream) {
+    const long long rows = diff_rows(a), keys = (long long)a.B * a.kv_heads * a.n_k;
     constexpr int LANES = W * (int)sizeof(T) / 16;
+    constexpr bool BF16 = sizeof(T) == 2;
     hipLaunchKernelGGL((diff_attn_rows_kernel<T, W>), dim3((unsigned)((rows * LANES + 255) / 256)), dim3(256), 0, stream, a);
     jv_status st = launch_status("diff_attn_rows_kernel");
     if (st != JV_OK) return st;
-    a.blocks = (a.n_k + 127) / 128;
-    a.items = (long long)a.B * a.kv_heads * a.blocks;
-    hipLaunchKernelGGL((diff_attn_dkv_kernel<T, W>), dim3(diff_grid(a.items)), dim3(256), 0, stream, a);
+    a.blocks = plan.k_blocks;
+    a.parts = plan.k_parts;
+    a.items = (long long)a.B * a.kv_heads * a.blocks * a.parts;
+    if constexpr (BF16) hipLaunchKernelGGL((diff_attn_dkv_bf16_kernel<W>), dim3(diff_grid(a.items)), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((diff_attn_dkv_f32_kernel<W>), dim3(diff_grid(a.items)), dim3(256), 0, stream, a);
     if ((st = launch_status("diff_attn_dkv_kernel")) != JV_OK) return st;
-    a.blocks = (a.n_q + 127) / 128;
-    a.items = (long long)a.B * a.heads * a.blocks;
-    hipLaunchKernelGGL((diff_attn_dq_kernel<T, W>), dim3(diff_grid(a.items)), dim3(256), 0, stream, a);
+    if (a.parts > 1) {
+        hipLaunchKernelGGL((diff_attn_sum_kernel<T, W>), dim3((unsigned)((keys * (W / 2) + 255) / 256)), dim3(256), 0, stream, (const float *)a.dkv_part, a.parts, keys,
+                           a.kv_heads, a.n_k, a.dk, a.dv, 2 * W);
+        if ((st = launch_status("diff_attn_sum_kernel")) != JV_OK) return st;
+    }
+    a.blocks = plan.q_blocks;
+    a.parts = plan.q_parts;
+    a.items = (long long)a.B * a.heads * a.blocks * a.parts;
+    if constexpr (BF16) hipLaunchKernelGGL((diff_attn_dq_bf16_kernel<W>), dim3(diff_grid(a.items)), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((diff_attn_dq_f32_kernel<W>), dim3(diff_grid(a.items)), dim3(256), 0, stream, a);
     if ((st = launch_status("diff_attn_dq_kernel")) != JV_OK) return st;
+    if (a.parts > 1) {
+        hipLaunchKernelGGL((diff_attn_sum_kernel<T, W>), dim3((unsigned)((rows * (W / 4) + 255) / 256)), dim3(256), 0, stream, (const float *)a.dq_part, a.parts, rows, a.heads,
+                           a.n_q, a.dq, a.dq, W);
+        if ((st = launch_status("diff_attn_sum_kernel")) != JV_OK) return st;
+    }
     if (!a.dlq1) return JV_OK;
     const int waves = a.l_step ? (a.heads < 16 ? a.heads : 16) : 16;
     hipLaunchKernelGGL((diff_attn_dlambda_kernel<W>), dim3(1), dim3(64 * waves), 0, stream, a);
     return launch_status("diff_attn_dlambda_kernel");
 }
-
-// Workspace: D1 and D2 of every row, then the sums for lambda of every block of 128 rows.
-static size_t diff_bwd_rows_bytes(const jv_diff_attn_desc *d) { return ((size_t)d->batch * d->heads * d->n_q * 8 + 255) & ~(size_t)255; }
 
 }  // namespace jv
 
@@ -401,8 +829,8 @@ extern "C" {
 size_t jv_diff_attn_bwd_workspace_bytes(const jv_diff_attn_desc *desc) {
     jv::clear_error();
     if (jv::diff_check_desc(desc) != JV_OK) return 0;
-    const size_t blocks = (size_t)desc->batch * desc->heads * ((desc->n_q + 127) / 128);
-    return jv::diff_bwd_rows_bytes(desc) + ((blocks * 4 + 255) & ~(size_t)255);
+    const jv::DiffBwdPlan plan = jv::diff_bwd_plan(desc);
+    return plan.stats + plan.lam + plan.dq + plan.dkv;
 }
 
 jv_status jv_diff_attn_bwd(const jv_diff_attn_desc *desc, const void *q, const void *k, const void *v,
@@ -444,7 +872,7 @@ jv_status jv_diff_attn_bwd(const jv_diff_attn_desc *desc, const void *q, const v
         return jv::fail(JV_ERR_WORKSPACE_TOO_SMALL, "saved holds %zu bytes, %zu are needed", saved_bytes, jv::diff_saved_bytes(desc));
     const size_t need = jv_diff_attn_bwd_workspace_bytes(desc);
     if (workspace_bytes < need) return jv::fail(JV_ERR_WORKSPACE_TOO_SMALL, "workspace holds %zu bytes, %zu are needed", workspace_bytes, need);
-    if (jv::diff_rows(p.a) * 32 > 0x7fffff00ll * 256 || (long long)B * H * (((long long)std::max(NQ, NK) + 127) / 128) > 0x7ffffff0ll)
+    if (jv::diff_rows(p.a) * 32 > 0x7fffff00ll * 256 || (long long)B * H * (((long long)std::max(NQ, NK) + 127) / 128) > 0x7fffff0ll)
         return jv::fail(JV_ERR_UNSUPPORTED, "more than 2^31 workgroups");
     auto arg = [](const void *ptr, const jv_strides &s) { return jv::TensorArg{ptr, s.stride_b, s.stride_h, s.stride_n}; };
     p.a.d_o = arg(grads->d_o, grads->d_o_strides);
@@ -456,11 +884,15 @@ jv_status jv_diff_attn_bwd(const jv_diff_attn_desc *desc, const void *q, const v
     p.a.dlq2 = grads->d_q2;
     p.a.dlk2 = grads->d_k2;
     jv::diff_use_saved(&p, const_cast<void *>(saved));
-    p.a.rows_d = (float *)workspace;
-    p.a.lam_part = (float *)((char *)workspace + jv::diff_bwd_rows_bytes(desc));
+    const jv::DiffBwdPlan plan = jv::diff_bwd_plan(desc);
+    char *at = (char *)workspace;
+    p.a.stats = (float *)at;
+    p.a.lam_part = (float *)(at += plan.stats);
+    p.a.dq_part = (float *)(at += plan.lam);
+    p.a.dkv_part = (float *)(at += plan.dq);
     return jv::diff_with_kind(p.bf16, W, [&](auto kind) {
         using K = decltype(kind);
-        return jv::diff_backward<typename K::T, K::W>(p.a, (hipStream_t)hip_stream);
+        return jv::diff_backward<typename K::T, K::W>(p.a, plan, (hipStream_t)hip_stream);
     });
 }
 

@@ -104,7 +104,7 @@ def test_types_saved_memory_and_workspaces_that_are_refused():
     for d in (desc(), desc(dtype=binding.JV_F32), desc(W=128)):
         work, saved, back = queries(d)
         rows, size = 2 * 4 * 50, 2 if d.dtype == binding.JV_BF16 else 4
-        assert saved >= rows * (8 + d.head_dim * size) and back >= rows * 8
+        assert saved >= rows * (16 + d.head_dim * size) and back >= rows * 16
         assert forward(d, saved=SAVED, saved_bytes=saved - 1) == SMALL and forward(d, saved=SAVED + 16, saved_bytes=saved) == INVALID
         assert backward(d, saved_bytes=saved - 1) == SMALL and backward(d, work_bytes=back - 1) == SMALL
         assert backward(d, saved=None) == INVALID and backward(d, work=None) == INVALID and backward(d, work=WORK + 64) == INVALID
