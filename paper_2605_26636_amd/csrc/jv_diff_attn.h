@@ -47,12 +47,29 @@ struct DiffProblem {
     bool bf16, o_bf16;
 };
 
-// Workgroup -> item: contiguous ranges per XCD (workgroup w runs on XCD w % 8), so that the workgroups of a (batch, head)
-// share its K and V in one L2.
-__device__ inline long long diff_item(long long items) {
-    const long long per = (items + 7) / 8;
-    return (long long)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-}
+// What a workgroup works on: a block of rows (or keys) of a (batch, head) and one of `parts` parts of it.  Without a mask, contiguous
+// ranges of (batch, head)s per XCD (workgroup w runs on XCD w % 8), so that the workgroups of one share its K and V in one L2.
+// Causal: the blocks with most work of all of them first (an XCD's (batch, head)s one after the other leave its last long
+// blocks alone at the end: forward pass of 2 x 4 096 tokens x 16 heads of 128 channels 291 us, now 236; where their number is a multiple of
+// 8 each stays on one XCD all the same).  False where a workgroup of the rounded-up grid has no work.
+struct DiffItem {
+    int part, block, bh;
+    __device__ bool find(const DiffArgs &a, int n_bh, int parts, bool last_block_first) {
+        long long item = blockIdx.x;
+        if (!a.causal) item = (blockIdx.x & 7) * ((a.items + 7) / 8) + (blockIdx.x >> 3);
+        if (item >= a.items) return false;
+        if (a.causal) {
+            bh = (int)(item % n_bh);
+            item /= n_bh;
+        }
+        part = (int)(item % parts);
+        item /= parts;
+        block = (int)(item % a.blocks);
+        if (!a.causal) bh = (int)(item / a.blocks);
+        if (last_block_first) block = a.blocks - 1 - block;
+        return true;
+    }
+};
 inline unsigned diff_grid(long long items) { return (unsigned)(8 * ((items + 7) / 8)); }
 
 constexpr int kDiffTile = 32;  // tokens of a tile

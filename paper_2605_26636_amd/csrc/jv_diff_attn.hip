@@ -90,12 +90,12 @@ struct DiffPlace {
     bool row_live;
     template <int WAVES, bool SPLIT>
     __device__ bool find(const DiffArgs &a, int wave, int li) {
-        long long item = diff_item(a.items);
-        if (item >= a.items) return false;
-        split = SPLIT ? (int)(item % a.splits) : 0;
-        if (SPLIT) item /= a.splits;
-        const int block = a.blocks - 1 - (int)(item % a.blocks);  // causal: the longest rows first
-        bkv = (int)(item / a.blocks);
+        DiffItem item;
+        if (!item.find(a, a.B * a.kv_heads, SPLIT ? a.splits : 1, true)) return false;
+        split = item.part;
+        bkv = item.bh;
+        // (causal: the last blocks of all heads of a group before the ones before them)
+        const int per_head = a.blocks / a.group, block = a.causal && per_head * a.group == a.blocks ? item.block % a.group * per_head + item.block / a.group : item.block;
         b = bkv / a.kv_heads;
         kv = bkv % a.kv_heads;
         n_rows = a.group * a.n_q;
@@ -459,12 +459,16 @@ __global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffA
     diff_finish<__bf16, TO, W, SPLIT>(a, place, w1, w2, l);
 }
 
-// The parts of a row joined, in their order: one wavefront a row.
-template <typename T, typename TO, int W>
+// The parts of a row joined by SHARE wavefronts, which take every SHARE-th part each, eight parts' loads at a time (parts that saw no key are
+// read, in bounds, and not used), and are added in their order.  Four wavefronts a row where there are many parts: one query token
+// against 16 384 keys x 8 sequences x 16 heads in 24 parts 6 us, in 39 with one wavefront and one part after the other 21;
+// 576 tokens x 24 heads in 4 parts 25 us with four wavefronts a row, 11 with one.
+template <typename T, typename TO, int W, int SHARE>
 __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
-    const int lane = threadIdx.x & 63, n_rows = a.group * a.n_q;
-    const long long all = (long long)a.B * a.kv_heads * n_rows, at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (at >= all) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, turn = wave % SHARE, n_rows = a.group * a.n_q;
+    const long long all = (long long)a.B * a.kv_heads * n_rows, at = (long long)blockIdx.x * (4 / SHARE) + wave / SHARE;
+    __shared__ float sums[4][2 * W];
+    if (SHARE == 1 && at >= all) return;
     const int bkv = (int)(at / n_rows), r = (int)(at % n_rows), b = bkv / a.kv_heads, kv = bkv % a.kv_heads;
     const int hg = r / a.n_q, qi = r - hg * a.n_q, head = kv * a.group + hg;
     f32x4 ml = {-INFINITY, 0.f, -INFINITY, 0.f};
@@ -478,28 +482,37 @@ __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
     const float f1 = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m1), f2 = ml[2] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[2] - m2);
     const float l1 = wave_sum(ml[1] * f1), l2 = wave_sum(ml[3] * f2);
     const unsigned long long seen = __builtin_amdgcn_ballot_w64(ml[0] != -INFINITY || ml[2] != -INFINITY);
-    constexpr int PER = W / 64;
-    float x1[PER] = {}, x2[PER] = {};
-    for (int s = 0; s < a.splits; ++s) {
-        if (!(seen >> s & 1)) continue;
-        const float *part = a.part + ((long long)s * all + at) * (2 * W + 4) + 4 + lane * PER;
-        const float g1 = __shfl(f1, s), g2 = __shfl(f2, s);
+    constexpr int PER = W / 32;  // channels a lane: lanes 0 .. 31 those of the first map, 32 .. 63 of the second
+    float x[PER] = {};
+    const float *part = a.part + at * (2 * W + 4) + 4 + lane * PER;
+#pragma unroll 8
+    for (int s = turn; s < a.splits; s += SHARE) {
+        float y[PER];
 #pragma unroll
-        for (int e = 0; e < PER; ++e) {
-            x1[e] = fmaf(part[e], g1, x1[e]);
-            x2[e] = fmaf(part[W + e], g2, x2[e]);
-        }
+        for (int e = 0; e < PER; ++e) y[e] = part[s * all * (2 * W + 4) + e];
+        const float f_first = __shfl(f1, s), f_second = __shfl(f2, s), f = lane < 32 ? f_first : f_second;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) x[e] = seen >> s & 1 ? fmaf(y[e], f, x[e]) : x[e];
     }
-    const float lam = diff_lambda<W>(a, head, lane).value;
-    const float inv1 = l1 > 0.f ? 1.f / l1 : l1, inv2 = l2 > 0.f ? 1.f / l2 : l2;
-    const long long row = ((long long)b * a.heads + head) * a.n_q + qi;
-    if (a.ml && lane == 0) diff_save(a, row, m1, l1, m2, l2);
-    TO *o = (TO *)const_cast<void *>(a.o.ptr) + b * a.o.sb + head * a.o.sh + qi * a.o.sn + lane * PER;
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-        const float y = x2[e] * inv2;
-        o[e] = (TO)fmaf(-lam, y, x1[e] * inv1);
-        if (a.o2) ((T *)a.o2)[row * W + lane * PER + e] = (T)y;
+    for (int e = 0; e < PER; ++e) sums[wave][lane * PER + e] = x[e];
+    const float lam = diff_lambda<W>(a, head, lane).value;
+    if (SHARE > 1) __syncthreads();
+    else __builtin_amdgcn_wave_barrier();  // (a wavefront's own LDS operations keep their order)
+    const long long row = ((long long)b * a.heads + head) * a.n_q + qi;
+    if (a.ml && turn == 0 && lane == 0) diff_save(a, row, m1, l1, m2, l2);
+    const float inv1 = l1 > 0.f ? 1.f / l1 : l1, inv2 = l2 > 0.f ? 1.f / l2 : l2;
+    TO *o = (TO *)const_cast<void *>(a.o.ptr) + b * a.o.sb + head * a.o.sh + qi * a.o.sn;
+    for (int ch = turn * 64 + lane; ch < W; ch += 64 * SHARE) {
+        float y1 = 0.f, y2 = 0.f;
+#pragma unroll
+        for (int w = 0; w < SHARE; ++w) {
+            y1 += sums[wave - turn + w][ch];
+            y2 += sums[wave - turn + w][W + ch];
+        }
+        y2 *= inv2;
+        o[ch] = (TO)fmaf(-lam, y2, y1 * inv1);
+        if (a.o2) ((T *)a.o2)[row * W + ch] = (T)y2;
     }
 }
 
@@ -509,17 +522,18 @@ __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
 
 // How a forward pass is cut: wavefronts a workgroup (32 rows each) and parts of the keys.  Up to 64 rows (a few queries, all heads
 // of a group together) take one wavefront each; more take workgroups of four, which share the tiles.  Keys are cut where
-// the launch would leave units idle: into as many parts as fill about two workgroups of four wavefronts a unit, of
-// four tiles at least, at most 64 (a wavefront of the join holds one part a lane).
+// the launch would leave units idle: into as many parts as the chip holds workgroups at a time (single wavefronts: three a unit
+// for their 48 KB of LDS; one query token against 16 384 keys x 8 sequences 53 us in 2 048 of them, 41 in 768), of four tiles at
+// least, at most 64 (a wavefront of the join holds one part a lane).
 struct DiffPlan {
     int waves, blocks, splits, tiles_per_split;
 };
-static DiffPlan diff_plan(int B, int kv_heads, long long n_rows, int n_k) {
+static DiffPlan diff_plan(int B, int kv_heads, long long n_rows, int n_k, bool bf16) {
     DiffPlan p;
     p.waves = n_rows <= 64 ? 1 : 4;
     p.blocks = (int)((n_rows + 32 * p.waves - 1) / (32 * p.waves));
     const long long groups = (long long)B * kv_heads * p.blocks, tiles = (n_k + kDiffTile - 1) / kDiffTile;
-    const long long want = p.waves == 1 ? 2048 : 512;
+    const long long want = p.waves == 1 ? 768 : bf16 ? 512 : 256;
     long long splits = groups * 2 > want ? 1 : want / groups;
     splits = std::max(1ll, std::min({splits, tiles / 4, 64ll}));
     p.tiles_per_split = (int)((tiles + splits - 1) / splits);
@@ -583,7 +597,7 @@ jv_status diff_check_desc(const jv_diff_attn_desc *d) {
 }
 
 static DiffPlan diff_plan_of(const jv_diff_attn_desc *d) {
-    return diff_plan(d->batch, d->kv_heads, (long long)d->heads / d->kv_heads * d->n_q, d->n_k);
+    return diff_plan(d->batch, d->kv_heads, (long long)d->heads / d->kv_heads * d->n_q, d->n_k, d->dtype == JV_BF16);
 }
 
 size_t diff_saved_bytes(const jv_diff_attn_desc *d) {
@@ -661,7 +675,9 @@ static jv_status diff_forward(DiffArgs a, const DiffPlan &plan, hipStream_t stre
     else launch(std::integral_constant<int, 4>(), std::true_type());
     const jv_status st = launch_status("diff_attn_fwd_kernel");
     if (st != JV_OK) return st;
-    hipLaunchKernelGGL((diff_attn_join_kernel<T, TO, W>), dim3((unsigned)((diff_rows(a) + 3) / 4)), dim3(256), 0, stream, a);
+    const long long rows = diff_rows(a);
+    if (a.splits > 8) hipLaunchKernelGGL((diff_attn_join_kernel<T, TO, W, 4>), dim3((unsigned)rows), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((diff_attn_join_kernel<T, TO, W, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a);
     return launch_status("diff_attn_join_kernel");
 }
 

@@ -55,15 +55,15 @@ __global__ void __launch_bounds__(256) diff_attn_rows_kernel(DiffArgs a) {
         d1 += __shfl_xor(d1, x);
         d2 += __shfl_xor(d2, x);
     }
-    if (!live || ch) return;
+    if (!live || ch >= 4 * PER) return;
     const long long n = diff_rows(a);
-    const bool there = qi < DiffLengths(a, b).q;
-    for (int m = 0; m < 2; ++m) {
-        const float ref = there ? a.ml[2 * m * n + row] : INFINITY;
-        a.stats[m * n + row] = ref == INFINITY ? -INFINITY : -(ref + log2f(a.ml[(2 * m + 1) * n + row])) / a.c;
+    const int which = ch / PER;  // a statistic a lane
+    if (which < 2) {
+        const float ref = qi < DiffLengths(a, b).q ? a.ml[2 * which * n + row] : INFINITY;
+        a.stats[which * n + row] = ref == INFINITY ? -INFINITY : -(ref + log2f(a.ml[(2 * which + 1) * n + row])) / a.c;
+    } else {
+        a.stats[which * n + row] = which == 2 ? -d1 : -lam * (d1 - d2);
     }
-    a.stats[2 * n + row] = -d1;
-    a.stats[3 * n + row] = -lam * (d1 - d2);
 }
 
 // One of a.parts equal parts of `total`: [from, to).
@@ -123,12 +123,11 @@ struct DiffQueries {
     long long row;
     bool row_live;
     __device__ bool find(const DiffArgs &a, int (&wave_most)[4], int wave, int lane) {
-        long long item = diff_item(a.items);
-        if (item >= a.items) return false;
-        part = (int)(item % a.parts);
-        item /= a.parts;
-        block = a.blocks - 1 - (int)(item % a.blocks);  // causal: the longest rows first
-        const int bh = (int)(item / a.blocks);
+        DiffItem item;
+        if (!item.find(a, a.B * a.heads, a.parts, true)) return false;
+        part = item.part;
+        block = item.block;
+        const int bh = item.bh;
         b = bh / a.heads;
         h = bh % a.heads;
         kv = h / a.group;
@@ -362,12 +361,11 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dq_bf16_kernel(DiffArgs a) {
 struct DiffKeys {
     int part, block, b, kv, key, shift, first_query, tile_begin, n_tiles, from, to, len_q, len_k;
     __device__ bool find(const DiffArgs &a, int wave, int lane) {
-        long long item = diff_item(a.items);
-        if (item >= a.items) return false;
-        part = (int)(item % a.parts);
-        item /= a.parts;
-        block = (int)(item % a.blocks);  // causal: the keys that most queries see first
-        const int bkv = (int)(item / a.blocks);
+        DiffItem item;
+        if (!item.find(a, a.B * a.kv_heads, a.parts, false)) return false;
+        part = item.part;
+        block = item.block;
+        const int bkv = item.bh;
         b = bkv / a.kv_heads;
         kv = bkv % a.kv_heads;
         const DiffLengths len(a, b);
