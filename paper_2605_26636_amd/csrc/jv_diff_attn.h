@@ -275,31 +275,38 @@ struct DiffLds {
 };
 
 // Loads of tiles into LDS by WAVES wavefronts, 1 KB an instruction: a lane fetches the chunk that belongs in its slot.  Rows at
-// `limit` and beyond are fetched as the one before it (the kernels mask them).
-template <int W, int WAVES>
+// `limit` and beyond are fetched as the one before it (the kernels mask them).  HELD: a lane's offsets are kept in registers, or worked
+// out at every load (a dozen instructions a tile, where registers are short).
+template <int W, int WAVES, bool HELD = true>
 struct DiffDma {
     using Tile = DiffTile<__bf16, W>;
     static constexpr int kLoads = kDiffTile * W / (512 * WAVES), kRows = 512 / W, kChunks = W / 8;
     const char *base;
     long long step;
-    unsigned off[kLoads];
+    unsigned off[HELD ? kLoads : 1];
     __device__ static unsigned chunk(int row, int slot) { return (Tile::off(row, slot) - row * 2 * W) / 16; }  // (its own inverse)
-    __device__ void start(const void *tensor, long long offset, long long sn, int wave, int lane) {
-        base = diff_uniform((const __bf16 *)tensor + offset);
+    __device__ unsigned offset(int i, int wave, int lane) const {
+        return (unsigned)(lane / kChunks) * (unsigned)step + 16 * chunk((wave * kLoads + i) * kRows + lane / kChunks, lane % kChunks);
+    }
+    __device__ void start(const void *tensor, long long offset_, long long sn, int wave, int lane) {
+        base = diff_uniform((const __bf16 *)tensor + offset_);
         step = 2 * sn;
+        if (HELD)
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) off[i] = (unsigned)(lane / kChunks) * (unsigned)step + 16 * chunk((wave * kLoads + i) * kRows + lane / kChunks, lane % kChunks);
+            for (int i = 0; i < kLoads; ++i) off[HELD ? i : 0] = offset(i, wave, lane);
     }
     __device__ void issue(unsigned char *tile, int row0, int limit, int wave, int lane) const {
         const char *from = base + row0 * step;
         if (row0 + kDiffTile <= limit) {  // (uniform)
+            if (!HELD) asm volatile("" : "+v"(lane));
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int first = (wave * kLoads + i) * kRows;
-                __builtin_amdgcn_global_load_lds((diff_global_cvoid *)(from + first * step + off[i]), (diff_lds_void *)(tile + first * 2 * W), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds((diff_global_cvoid *)(from + first * step + (HELD ? off[HELD ? i : 0] : offset(i, wave, lane))),
+                                                 (diff_lds_void *)(tile + first * 2 * W), 16, 0, 0);
             }
         } else {
-            asm("" : "+v"(lane));  // (worked out here: in registers all the way they would be missed)
+            asm volatile("" : "+v"(lane));
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int first = (wave * kLoads + i) * kRows, row = first + lane / kChunks;

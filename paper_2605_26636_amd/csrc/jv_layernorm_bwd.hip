@@ -20,7 +20,9 @@ struct NormGradArgs {
     float eps;
 };
 
-constexpr int kNormGradMostGroups = 1024;
+// Workgroups of a launch at most (each leaves column sums to be added), and their threads.  32 768 x 1024 in bf16 with a residual 50 us with 1 024
+// of 256 threads, 46 with these: half the sums.
+constexpr int kNormGradMostGroups = 512, kNormGradThreads = 512;
 
 // Eight columns from an element on.
 template <bool BF16>
@@ -76,30 +78,34 @@ __device__ inline float norm_sum(float x) {
     return x;
 }
 
-// LANES lanes a row (256: a whole workgroup), NV pieces of eight columns a lane: piece p of lane l is columns 8 (l + LANES p) .. + 7.
+// LANES lanes a row, NV pieces of eight columns a lane: piece p of lane l is columns 8 (l + LANES p) .. + 7.  At most two pieces, so
+// that two workgroups share a unit: rows of more than 1 024 columns lie in two to eight wavefronts, which join their sums through LDS (three or four pieces
+// in one wavefront, or in four with half the wavefronts a unit: 20 000 x 1280 in bf16 61 us, 16 000 x 2560 113).
 template <bool X_BF16, bool DY_BF16, int LANES, int NV>
-__global__ void __launch_bounds__(256) layernorm_bwd_kernel(NormGradArgs a) {
-    constexpr int ROWS = 256 / LANES;  // of a workgroup at a time
+__global__ void __launch_bounds__(kNormGradThreads) layernorm_bwd_kernel(NormGradArgs a) {
+    constexpr int THREADS = kNormGradThreads, ROWS = THREADS / LANES;  // rows of a workgroup at a time
+    constexpr int ROW_WAVES = LANES > 64 ? LANES / 64 : 1, GROUPS = LANES > 64 ? ROWS : THREADS / 64;  // wavefronts of a row; column sums of a workgroup
     const int tid = threadIdx.x, lane = tid % LANES, wave = tid >> 6;
-    __shared__ float across[2][2][4];
-    __shared__ __align__(16) float column[LANES == 256 ? 4 : 4 * 64 * 8];
+    __shared__ float across[2][2][THREADS / 64];
+    __shared__ __align__(16) float column[GROUPS * 8 * LANES];
     const float inv_cols = 1.0f / (float)a.cols;
     int turn = 0;
     // both sums over the lanes of a row
     auto sums = [&](float &x, float &y) {
-        if constexpr (LANES <= 64) {
-            x = norm_sum<LANES>(x);
-            y = norm_sum<LANES>(y);
-        } else {
-            x = norm_sum<64>(x);
-            y = norm_sum<64>(y);
+        x = norm_sum<(LANES < 64 ? LANES : 64)>(x);
+        y = norm_sum<(LANES < 64 ? LANES : 64)>(y);
+        if constexpr (ROW_WAVES > 1) {
             if ((tid & 63) == 0) {
                 across[turn][0][wave] = x;
                 across[turn][1][wave] = y;
             }
             __syncthreads();
-            x = (across[turn][0][0] + across[turn][0][1]) + (across[turn][0][2] + across[turn][0][3]);
-            y = (across[turn][1][0] + across[turn][1][1]) + (across[turn][1][2] + across[turn][1][3]);
+            x = y = 0.f;
+#pragma unroll
+            for (int w = 0; w < ROW_WAVES; ++w) {
+                x += across[turn][0][wave / ROW_WAVES * ROW_WAVES + w];
+                y += across[turn][1][wave / ROW_WAVES * ROW_WAVES + w];
+            }
             turn ^= 1;  // (the next sums are written elsewhere: one barrier each suffices)
         }
     };
@@ -177,26 +183,23 @@ __global__ void __launch_bounds__(256) layernorm_bwd_kernel(NormGradArgs a) {
 #pragma unroll
         for (int p = 0; p < NV; ++p) {
             float(&v)[8] = which ? dbeta[p] : dgamma[p];
-            const int c = 8 * (lane + LANES * p);
-            if constexpr (LANES == 256) {
-                if (c < a.cols) norm_store8<false>(part, (size_t)which * a.cols + c, v);
-            } else {
-                // rows of a wavefront (every LANES-th lane), then the four wavefronts
+            // rows of a wavefront (every LANES-th lane), then those of the workgroup
 #pragma unroll
-                for (int x = LANES; x < 64; x *= 2)
+            for (int x = LANES; x < 64; x *= 2)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] += __shfl_xor(v[e], x);
-                __syncthreads();
-                if ((tid & 63) < LANES) {
+                for (int e = 0; e < 8; ++e) v[e] += __shfl_xor(v[e], x);
+            __syncthreads();
+            if (LANES >= 64 || (tid & 63) < LANES) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) column[(wave * 8 + e) * 64 + lane] = v[e];
-                }
-                __syncthreads();
-                for (int y = tid; y < 8 * LANES; y += 256) {
-                    const int e = y / LANES, l = y % LANES, to = 8 * (l + LANES * p) + e;
-                    const float s = (column[e * 64 + l] + column[(8 + e) * 64 + l]) + (column[(16 + e) * 64 + l] + column[(24 + e) * 64 + l]);
-                    if (to < a.cols) part[(size_t)which * a.cols + to] = s;
-                }
+                for (int e = 0; e < 8; ++e) column[((LANES > 64 ? tid / LANES : wave) * 8 + e) * LANES + lane] = v[e];
+            }
+            __syncthreads();
+            for (int y = tid; y < 8 * LANES; y += THREADS) {
+                const int e = y / LANES, l = y % LANES, to = 8 * (l + LANES * p) + e;
+                float s = 0.f;
+#pragma unroll
+                for (int w = 0; w < GROUPS; ++w) s += column[(w * 8 + e) * LANES + l];
+                if (to < a.cols) part[(size_t)which * a.cols + to] = s;
             }
         }
 }
@@ -208,7 +211,7 @@ __global__ void __launch_bounds__(1024) layernorm_bwd_columns_kernel(const float
     __shared__ float sums[16][64];
     float sum = 0.f;
     if (c < 2 * cols)
-#pragma unroll 8
+#pragma unroll 16
         for (int p = wave; p < n; p += 16) sum += part[(size_t)p * 2 * cols + c];
     sums[wave][lane] = sum;
     __syncthreads();
@@ -223,29 +226,28 @@ __global__ void __launch_bounds__(1024) layernorm_bwd_columns_kernel(const float
 template <typename F>
 static void norm_with_row(int cols, F f) {
     const int pieces = cols / 8;
-    auto lanes = [&](auto l) {
-        constexpr int L = decltype(l)::value;
-        const int nv = (pieces + L - 1) / L;
-        if (nv <= 1) f(l, std::integral_constant<int, 1>());
-        else if (nv <= 2) f(l, std::integral_constant<int, 2>());
-        else if (nv <= 3) f(l, std::integral_constant<int, 3>());
-        else f(l, std::integral_constant<int, 4>());
-    };
-    if (pieces <= 8) f(std::integral_constant<int, 8>(), std::integral_constant<int, 1>());
-    else if (pieces <= 16) f(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
-    else if (pieces <= 32) f(std::integral_constant<int, 32>(), std::integral_constant<int, 1>());
-    else if (pieces > 64 && pieces <= 96) f(std::integral_constant<int, 32>(), std::integral_constant<int, 3>());
-    else if (pieces <= 256) lanes(std::integral_constant<int, 64>());
-    else lanes(std::integral_constant<int, 256>());
+    using One = std::integral_constant<int, 1>;
+    using Two = std::integral_constant<int, 2>;
+    if (pieces <= 8) f(std::integral_constant<int, 8>(), One());
+    else if (pieces <= 16) f(std::integral_constant<int, 16>(), One());
+    else if (pieces <= 32) f(std::integral_constant<int, 32>(), One());
+    else if (pieces <= 64) f(std::integral_constant<int, 64>(), One());
+    else if (pieces <= 128) f(std::integral_constant<int, 64>(), Two());
+    else if (pieces <= 256) f(std::integral_constant<int, 128>(), Two());
+    else if (pieces <= 512) f(std::integral_constant<int, 256>(), Two());
+    else f(std::integral_constant<int, 512>(), Two());
 }
 
+// Workgroups: one a step of rows up to 256 (one a unit), above that two steps each up to 512, since every workgroup's column sums are written and
+// read again (2 000 x 2048 in bf16: 500 workgroups of one step 20.0 us, 250 of two 14.8), then 512.
 static long long norm_groups(long long rows, int cols) {
-    long long groups = 0;
+    long long steps = 0;
     norm_with_row(cols, [&](auto lanes, auto) {
-        const int per = 256 / decltype(lanes)::value;
-        groups = (rows + per - 1) / per;
+        constexpr int per = kNormGradThreads / decltype(lanes)::value;
+        steps = (rows + per - 1) / per;
     });
-    return groups < kNormGradMostGroups ? groups : kNormGradMostGroups;
+    if (steps <= 256) return steps;
+    return steps <= kNormGradMostGroups ? (steps + 1) / 2 : kNormGradMostGroups;
 }
 
 static jv_status norm_check_sizes(int64_t rows, int32_t cols) {
@@ -298,7 +300,7 @@ jv_status jv_layernorm_bwd(const void *x, const float *gamma, const void *dy, co
         constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value;
         auto kernel = x_dtype == JV_BF16 ? (dy_dtype == JV_BF16 ? jv::layernorm_bwd_kernel<true, true, L, NV> : jv::layernorm_bwd_kernel<true, false, L, NV>)
                                          : (dy_dtype == JV_BF16 ? jv::layernorm_bwd_kernel<false, true, L, NV> : jv::layernorm_bwd_kernel<false, false, L, NV>);
-        hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL(kernel, dim3(groups), dim3(jv::kNormGradThreads), 0, stream, a);
     });
     if ((st = jv::launch_status("layernorm_bwd_kernel")) != JV_OK || !dgamma) return st;
     hipLaunchKernelGGL(jv::layernorm_bwd_columns_kernel, dim3((2 * cols + 63) / 64), dim3(1024), 0, stream, (const float *)workspace, groups, cols, dgamma, dbeta);
