@@ -353,10 +353,10 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _same_device(first, *others):
-    for t in (first,) + others:
-        if t is not None and (not t.is_cuda or t.device != first.device):
-            raise ValueError("tensors must live on one GPU")
+def _same_device(*tensors):
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != torch.cuda.current_device()):
+            raise ValueError("tensors must live on the current GPU")
 
 
 def _diff_lambda(lam, init, q):
@@ -365,12 +365,12 @@ def _diff_lambda(lam, init, q):
     shape = tuple(lam[0].shape)
     if len(lam) != 4 or shape not in shapes:
         raise ValueError("lambda has four vectors, each [head_dim / 2] or [heads, head_dim / 2]")
-    _check_vectors(lam, shape, q)
+    _check_vectors(lam, shape)
     return JvDiffLambda(*[t.data_ptr() for t in lam], init, 1 if len(shape) == 2 else 0)
 
 
-def _check_vectors(vectors, shape, q):
-    _same_device(q, *vectors)
+def _check_vectors(vectors, shape):
+    _same_device(*vectors)
     for t in vectors:
         if t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape) != shape:
             raise ValueError("lambda's vectors and their gradients must be contiguous fp32 tensors of one shape")
@@ -396,13 +396,16 @@ def jv_diff_attn_fwd(q, k, v, lam, o, lambda_init=0.8, scale=0.0, causal=False, 
                      workspace=None, stream=None):
     """o <- differential attention of (q, k, v); lam: four fp32 tensors [d] or [heads, d], d = head_dim / 2.  saved: a tensor of
     jv_diff_attn_saved_bytes bytes that receives what the gradient needs.  Returns the workspace tensor used."""
-    desc = make_diff_desc(q, k, v, o, causal, q_lengths, k_lengths)
     if workspace is None:
+        desc = make_diff_desc(q, k, v, o, causal, q_lengths, k_lengths)
         workspace = torch.empty(max(jv_diff_attn_workspace_bytes(desc), 256), dtype=torch.uint8, device=q.device)
-    _same_device(q, saved, workspace)
-    _check(lib().jv_diff_attn_fwd(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                  ctypes.byref(_diff_lambda(lam, lambda_init, q)), o.data_ptr(), scale, *_sized(saved),
-                                  *_sized(workspace), _stream(stream)))
+    st = (_native or _load_native()).diff_attn_fwd(q, k, v, lam, o, lambda_init, scale, causal, q_lengths, k_lengths, saved, workspace, stream)
+    if st is None:
+        desc = make_diff_desc(q, k, v, o, causal, q_lengths, k_lengths)
+        _same_device(saved, workspace)
+        st = lib().jv_diff_attn_fwd(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), ctypes.byref(_diff_lambda(lam, lambda_init, q)),
+                                    o.data_ptr(), scale, *_sized(saved), *_sized(workspace), _stream(stream))
+    _check(st)
     return workspace
 
 
@@ -410,22 +413,27 @@ def jv_diff_attn_bwd(q, k, v, lam, o, saved, d_o, d_q, d_k, d_v, d_lam=None, lam
                      q_lengths=None, k_lengths=None, workspace=None, stream=None):
     """d_q, d_k, d_v and d_lam (four tensors like lam, or None) <- the gradient of jv_diff_attn_fwd, whose other arguments
     are given as they were there; returns the workspace tensor used."""
-    desc = make_diff_desc(q, k, v, o, causal, q_lengths, k_lengths)
-    for like, t in ((q, d_o), (q, d_q), (k, d_k), (v, d_v)):
-        if tuple(t.shape) != tuple(like.shape) or t.dtype != q.dtype:
-            raise ValueError("gradients must have the shape and dtype of their tensors")
-    _same_device(q, saved, d_o, d_q, d_k, d_v, workspace)
-    lam_arg = _diff_lambda(lam, lambda_init, q)
-    if d_lam is not None:
-        if len(d_lam) != 4:
-            raise ValueError("lambda has four vectors")
-        _check_vectors(d_lam, tuple(lam[0].shape), q)
     if workspace is None:
+        desc = make_diff_desc(q, k, v, o, causal, q_lengths, k_lengths)
         workspace = torch.empty(max(jv_diff_attn_bwd_workspace_bytes(desc), 256), dtype=torch.uint8, device=q.device)
-    grads = JvDiffAttnGrads(d_o.data_ptr(), d_q.data_ptr(), d_k.data_ptr(), d_v.data_ptr(), _strides(d_o), _strides(d_q), _strides(d_k),
-                            _strides(d_v), *([t.data_ptr() for t in d_lam] if d_lam is not None else [None] * 4))
-    _check(lib().jv_diff_attn_bwd(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), ctypes.byref(lam_arg), o.data_ptr(),
-                                  *_sized(saved), ctypes.byref(grads), scale, *_sized(workspace), _stream(stream)))
+    st = (_native or _load_native()).diff_attn_bwd(q, k, v, lam, o, saved, d_o, d_q, d_k, d_v, d_lam, lambda_init, scale, causal, q_lengths,
+                                                   k_lengths, workspace, stream)
+    if st is None:
+        desc = make_diff_desc(q, k, v, o, causal, q_lengths, k_lengths)
+        for like, t in ((q, d_o), (q, d_q), (k, d_k), (v, d_v)):
+            if tuple(t.shape) != tuple(like.shape) or t.dtype != q.dtype:
+                raise ValueError("gradients must have the shape and dtype of their tensors")
+        _same_device(saved, d_o, d_q, d_k, d_v, workspace)
+        lam_arg = _diff_lambda(lam, lambda_init, q)
+        if d_lam is not None:
+            if len(d_lam) != 4:
+                raise ValueError("lambda has four vectors")
+            _check_vectors(d_lam, tuple(lam[0].shape))
+        grads = JvDiffAttnGrads(d_o.data_ptr(), d_q.data_ptr(), d_k.data_ptr(), d_v.data_ptr(), _strides(d_o), _strides(d_q), _strides(d_k),
+                                _strides(d_v), *([t.data_ptr() for t in d_lam] if d_lam is not None else [None] * 4))
+        st = lib().jv_diff_attn_bwd(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), ctypes.byref(lam_arg), o.data_ptr(),
+                                    *_sized(saved), ctypes.byref(grads), scale, *_sized(workspace), _stream(stream))
+    _check(st)
     return workspace
 
 
@@ -478,19 +486,22 @@ def jv_layernorm_bwd(x, gamma, dy, dx, dgamma=None, dbeta=None, eps=1e-6, residu
     neither); x, dx and residual of one type, dy fp32 or bf16, all [rows, cols], gamma, dgamma, dbeta fp32 [cols].
     Returns the workspace tensor used."""
     rows, cols = x.shape
-    _same_device(x, gamma, dy, dx, dgamma, dbeta, residual, workspace)
-    for t in (x, dy, dx, residual):
-        if t is not None and not (t.is_contiguous() and tuple(t.shape) == (rows, cols)):
-            raise ValueError("x, dy, dx and residual must be contiguous [rows, cols]")
-    if dx.dtype != x.dtype or (residual is not None and residual.dtype != x.dtype):
-        raise TypeError("dx and residual must have x's dtype")
-    for t in (gamma, dgamma, dbeta):
-        if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape) != (cols,)):
-            raise ValueError("gamma, dgamma and dbeta must be contiguous fp32 [cols]")
     if workspace is None:
         workspace = torch.empty(max(jv_layernorm_bwd_workspace_bytes(rows, cols), 256), dtype=torch.uint8, device=x.device)
-    _check(lib().jv_layernorm_bwd(x.data_ptr(), gamma.data_ptr(), dy.data_ptr(), _ptr(residual), dx.data_ptr(), _ptr(dgamma), _ptr(dbeta),
-                                  rows, cols, eps, _dtype_code(x), _dtype_code(dy), *_sized(workspace), _stream(stream)))
+    st = (_native or _load_native()).layernorm_bwd(x, gamma, dy, dx, dgamma, dbeta, eps, residual, workspace, stream)
+    if st is None:
+        _same_device(x, gamma, dy, dx, dgamma, dbeta, residual, workspace)
+        for t in (x, dy, dx, residual):
+            if t is not None and not (t.is_contiguous() and tuple(t.shape) == (rows, cols)):
+                raise ValueError("x, dy, dx and residual must be contiguous [rows, cols]")
+        if dx.dtype != x.dtype or (residual is not None and residual.dtype != x.dtype):
+            raise TypeError("dx and residual must have x's dtype")
+        for t in (gamma, dgamma, dbeta):
+            if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or tuple(t.shape) != (cols,)):
+                raise ValueError("gamma, dgamma and dbeta must be contiguous fp32 [cols]")
+        st = lib().jv_layernorm_bwd(x.data_ptr(), gamma.data_ptr(), dy.data_ptr(), _ptr(residual), dx.data_ptr(), _ptr(dgamma), _ptr(dbeta),
+                                    rows, cols, eps, _dtype_code(x), _dtype_code(dy), *_sized(workspace), _stream(stream))
+    _check(st)
     return workspace
 
 

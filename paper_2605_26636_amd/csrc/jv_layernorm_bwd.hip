@@ -210,9 +210,14 @@ __global__ void __launch_bounds__(1024) layernorm_bwd_columns_kernel(const float
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
     __shared__ float sums[16][64];
     float sum = 0.f;
-    if (c < 2 * cols)
-#pragma unroll 16
-        for (int p = wave; p < n; p += 16) sum += part[(size_t)p * 2 * cols + c];
+    const float *column = part + min(c, 2 * cols - 1);
+    for (int p0 = wave; p0 < n; p0 += 256) {  // sixteen loads at a time, also where fewer are left (of the last part again, not added)
+        float x[16];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) x[u] = column[(size_t)min(p0 + 16 * u, n - 1) * 2 * cols];
+#pragma unroll
+        for (int u = 0; u < 16; ++u) sum += p0 + 16 * u < n ? x[u] : 0.f;
+    }
     sums[wave][lane] = sum;
     __syncthreads();
     if (wave || c >= 2 * cols) return;
@@ -238,8 +243,9 @@ static void norm_with_row(int cols, F f) {
     else f(std::integral_constant<int, 512>(), Two());
 }
 
-// Workgroups: one a step of rows up to 256 (one a unit), above that two steps each up to 512, since every workgroup's column sums are written and
-// read again (2 000 x 2048 in bf16: 500 workgroups of one step 20.0 us, 250 of two 14.8), then 512.
+// Workgroups: one a step of rows up to 256 (one a unit), then two steps each, 256 up to 1 024 steps, above that 512: every workgroup's column sums
+// are written and read again, which more of them must earn.  256 / 512 workgroups, us, in bf16 with a residual: 1 000 x 8192 (1 000
+// steps) 33 / 41, 6 000 x 1024 (750) 17.3 / 17.3 (without residual 13.2 / 15.7), 5 000 x 1280 (1 250) 28.1 / 23.2, 16 000 x 2048 (4 000) 84 / 59.
 static long long norm_groups(long long rows, int cols) {
     long long steps = 0;
     norm_with_row(cols, [&](auto lanes, auto) {
@@ -247,7 +253,7 @@ static long long norm_groups(long long rows, int cols) {
         steps = (rows + per - 1) / per;
     });
     if (steps <= 256) return steps;
-    return steps <= kNormGradMostGroups ? (steps + 1) / 2 : kNormGradMostGroups;
+    return steps <= 512 ? (steps + 1) / 2 : steps <= 1024 ? 256 : kNormGradMostGroups;
 }
 
 static jv_status norm_check_sizes(int64_t rows, int32_t cols) {

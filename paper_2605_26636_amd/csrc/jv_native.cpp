@@ -1,4 +1,4 @@
-// Argument marshalling of the token-mixer calls for Python: checks the tensors, fills the
+// Argument marshalling of the token-mixer calls, and of the gradients, for Python: checks the tensors, fills the
 // descriptor and calls the C entry points of libjetvit.so.  Host time of a call, launches included,
 // through ctypes structures / here: window or full attention 10.3 / 3.9 us, linear attention
 // 13.7 / 7.4 us, the block with generated filters 25.4 / 20.3 us, where the kernels of a small problem take about 10.
@@ -10,6 +10,7 @@
 #include <Python.h>
 
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
+#include <c10/hip/HIPFunctions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "jetvit.h"
@@ -187,6 +188,158 @@ PyObject *full_attn_fwd(PyObject *const *a) {
     return status_of([&] { return jv_full_attn_fwd(&c.desc, c.q, c.k, c.v, c.o, scale, c.stream); });
 }
 
+// A tensor on the current device of `like`'s element type (like = null: any); None allowed where `absent` is given.
+const at::Tensor *device_tensor(PyObject *obj, const at::Tensor *like, bool *absent = nullptr) {
+    if (absent) {
+        *absent = obj == Py_None;
+        if (*absent) return nullptr;
+    }
+    const at::Tensor *t = tensor_arg(obj);
+    return t && t->is_cuda() && t->get_device() == c10::hip::current_device() && (!like || t->scalar_type() == like->scalar_type()) ? t : nullptr;
+}
+bool bool_arg(PyObject *obj, bool *out) {
+    const int x = PyObject_IsTrue(obj);
+    *out = x > 0;
+    return x >= 0;
+}
+// Memory of a number of bytes, or None.
+bool memory_arg(PyObject *obj, void **ptr, size_t *bytes) {
+    bool absent;
+    const at::Tensor *t = device_tensor(obj, nullptr, &absent);
+    *ptr = t ? t->data_ptr() : nullptr;
+    *bytes = t ? t->nbytes() : 0;
+    return t || absent;
+}
+bool strided_arg(const at::Tensor *t, jv_strides *out, const at::Tensor *like = nullptr) {
+    if (!t || t->dim() != 4 || t->stride(3) != 1 || (like && t->sizes() != like->sizes())) return false;
+    *out = {t->stride(0), t->stride(1), t->stride(2)};
+    return true;
+}
+bool lengths_arg(PyObject *obj, int64_t batch, const int32_t **out) {
+    bool absent;
+    const at::Tensor *t = device_tensor(obj, nullptr, &absent);
+    *out = t ? (const int32_t *)t->data_ptr() : nullptr;
+    return absent || (t && t->scalar_type() == at::kInt && t->dim() == 1 && t->size(0) == batch && t->is_contiguous());
+}
+// Four contiguous fp32 vectors of one shape.
+bool vectors_arg(PyObject *obj, c10::IntArrayRef *shape, const float *(&out)[4], bool first) {
+    PyObject **items = items_arg(obj, 4);
+    if (!items) return false;
+    for (int i = 0; i < 4; ++i) {
+        const at::Tensor *t = device_tensor(items[i], nullptr);
+        if (!t || t->scalar_type() != at::kFloat || !t->is_contiguous()) return false;
+        if (first && i == 0) *shape = t->sizes();
+        if (t->sizes() != *shape) return false;
+        out[i] = (const float *)t->data_ptr();
+    }
+    return true;
+}
+
+struct DiffCall {
+    jv_diff_attn_desc desc;
+    jv_diff_lambda lambda;
+    const at::Tensor *q, *k, *v, *o;
+    c10::IntArrayRef shape;
+    float scale;
+    void *stream;
+};
+// args: q, k, v, lam, o; lambda_init, scale, causal, q_lengths, k_lengths; stream
+bool diff_args(PyObject *const *a, PyObject *const *more, PyObject *stream, DiffCall *c) {
+    c->desc = {};
+    jv_diff_attn_desc &d = c->desc;
+    bool causal;
+    if (!(c->q = device_tensor(a[0], nullptr)) || !(c->k = device_tensor(a[1], c->q)) || !(c->v = device_tensor(a[2], c->q)) || !(c->o = device_tensor(a[4], nullptr)) ||
+        !strided_arg(c->q, &d.q) || !strided_arg(c->k, &d.k) || !strided_arg(c->v, &d.v, c->k) || !strided_arg(c->o, &d.o, c->q) ||
+        !dtype_code(*c->q, &d.dtype) || !dtype_code(*c->o, &d.o_dtype) || !float_arg(more[0], &c->lambda.init) || !float_arg(more[1], &c->scale) ||
+        !bool_arg(more[2], &causal) || !lengths_arg(more[3], c->q->size(0), &d.q_lengths) || !lengths_arg(more[4], c->q->size(0), &d.k_lengths))
+        return false;
+    const auto q = c->q->sizes(), k = c->k->sizes();
+    if (k[0] != q[0] || k[3] != q[3]) return false;
+    for (int64_t x : {q[0], q[1], q[2], q[3], k[1], k[2]})
+        if (x != (int32_t)x) return false;
+    d.batch = (int32_t)q[0];
+    d.heads = (int32_t)q[1];
+    d.kv_heads = (int32_t)k[1];
+    d.n_q = (int32_t)q[2];
+    d.n_k = (int32_t)k[2];
+    d.head_dim = (int32_t)q[3];
+    d.causal = causal;
+    const float *vec[4];
+    if (!vectors_arg(a[3], &c->shape, vec, true)) return false;
+    const int64_t half = q[3] / 2;
+    if (!(c->shape == c10::IntArrayRef({half}) || c->shape == c10::IntArrayRef({q[1], half}))) return false;
+    c->lambda.q1 = vec[0];
+    c->lambda.k1 = vec[1];
+    c->lambda.q2 = vec[2];
+    c->lambda.k2 = vec[3];
+    c->lambda.per_head = c->shape.size() == 2;
+    return stream_arg(stream, &c->stream);
+}
+
+// (q, k, v, lam, o, lambda_init, scale, causal, q_lengths, k_lengths, saved, workspace, stream)
+PyObject *diff_attn_fwd(PyObject *const *a) {
+    DiffCall c;
+    void *saved, *ws;
+    size_t saved_bytes, bytes;
+    if (!diff_args(a, a + 5, a[12], &c) || !memory_arg(a[10], &saved, &saved_bytes) || !memory_arg(a[11], &ws, &bytes)) return nullptr;
+    return status_of([&] {
+        return jv_diff_attn_fwd(&c.desc, c.q->data_ptr(), c.k->data_ptr(), c.v->data_ptr(), &c.lambda, c.o->data_ptr(), c.scale, saved, saved_bytes, ws, bytes, c.stream);
+    });
+}
+
+// (q, k, v, lam, o, saved, d_o, d_q, d_k, d_v, d_lam, lambda_init, scale, causal, q_lengths, k_lengths, workspace, stream)
+PyObject *diff_attn_bwd(PyObject *const *a) {
+    DiffCall c;
+    jv_diff_attn_grads g = {};
+    void *saved, *ws;
+    size_t saved_bytes, bytes;
+    if (!diff_args(a, a + 11, a[17], &c) || !memory_arg(a[5], &saved, &saved_bytes) || !memory_arg(a[16], &ws, &bytes)) return nullptr;
+    const at::Tensor *d_o = device_tensor(a[6], c.q), *d_q = device_tensor(a[7], c.q), *d_k = device_tensor(a[8], c.q), *d_v = device_tensor(a[9], c.q);
+    if (!strided_arg(d_o, &g.d_o_strides, c.q) || !strided_arg(d_q, &g.d_q_strides, c.q) || !strided_arg(d_k, &g.d_k_strides, c.k) || !strided_arg(d_v, &g.d_v_strides, c.v))
+        return nullptr;
+    g.d_o = d_o->data_ptr();
+    g.d_q = d_q->data_ptr();
+    g.d_k = d_k->data_ptr();
+    g.d_v = d_v->data_ptr();
+    if (a[10] != Py_None) {
+        const float *vec[4];
+        if (!vectors_arg(a[10], &c.shape, vec, false)) return nullptr;
+        g.d_q1 = (float *)vec[0];
+        g.d_k1 = (float *)vec[1];
+        g.d_q2 = (float *)vec[2];
+        g.d_k2 = (float *)vec[3];
+    }
+    return status_of([&] {
+        return jv_diff_attn_bwd(&c.desc, c.q->data_ptr(), c.k->data_ptr(), c.v->data_ptr(), &c.lambda, c.o->data_ptr(), saved, saved_bytes, &g, c.scale, ws, bytes, c.stream);
+    });
+}
+
+// (x, gamma, dy, dx, dgamma, dbeta, eps, residual, workspace, stream)
+PyObject *layernorm_bwd(PyObject *const *a) {
+    bool no_dgamma, no_dbeta, no_residual;
+    const at::Tensor *x = device_tensor(a[0], nullptr), *gamma = device_tensor(a[1], nullptr), *dy = device_tensor(a[2], nullptr);
+    if (!x || !gamma || !dy) return nullptr;
+    const at::Tensor *dx = device_tensor(a[3], x), *dgamma = device_tensor(a[4], gamma, &no_dgamma), *dbeta = device_tensor(a[5], gamma, &no_dbeta);
+    const at::Tensor *residual = device_tensor(a[7], x, &no_residual);
+    if (!dx || !(dgamma || no_dgamma) || !(dbeta || no_dbeta) || !(residual || no_residual) || x->dim() != 2 || gamma->scalar_type() != at::kFloat) return nullptr;
+    for (const at::Tensor *t : {x, dy, dx, residual})
+        if (t && (!t->is_contiguous() || t->sizes() != x->sizes())) return nullptr;
+    const int64_t rows = x->size(0), cols = x->size(1);
+    for (const at::Tensor *t : {gamma, dgamma, dbeta})
+        if (t && (!t->is_contiguous() || t->sizes() != c10::IntArrayRef({cols}))) return nullptr;
+    jv_dtype x_type, dy_type;
+    float eps;
+    void *ws, *stream;
+    size_t bytes;
+    if (cols != (int32_t)cols || !dtype_code(*x, &x_type) || !dtype_code(*dy, &dy_type) || !float_arg(a[6], &eps) || !memory_arg(a[8], &ws, &bytes) || !stream_arg(a[9], &stream))
+        return nullptr;
+    auto ptr = [](const at::Tensor *t) { return t ? t->data_ptr() : nullptr; };
+    return status_of([&] {
+        return jv_layernorm_bwd(x->data_ptr(), (const float *)gamma->data_ptr(), dy->data_ptr(), ptr(residual), dx->data_ptr(), (float *)ptr(dgamma), (float *)ptr(dbeta), rows,
+                                (int32_t)cols, eps, x_type, dy_type, ws, bytes, stream);
+    });
+}
+
 // Tensors without memory of their own (under tracing or vmap) throw where their pointer or strides
 // are asked for, and torch where it has no device for the current stream: left to binding.py too.
 // Nothing throws behind an entry point, so no call is made twice.
@@ -209,6 +362,9 @@ PyMethodDef methods[] = {
     {"linear_block_fwd", (PyCFunction)(void *)guarded<linear_block_fwd, 13>, METH_FASTCALL, nullptr},
     {"window_attn_fwd", (PyCFunction)(void *)guarded<window_attn_fwd, 8>, METH_FASTCALL, nullptr},
     {"full_attn_fwd", (PyCFunction)(void *)guarded<full_attn_fwd, 7>, METH_FASTCALL, nullptr},
+    {"diff_attn_fwd", (PyCFunction)(void *)guarded<diff_attn_fwd, 13>, METH_FASTCALL, nullptr},
+    {"diff_attn_bwd", (PyCFunction)(void *)guarded<diff_attn_bwd, 18>, METH_FASTCALL, nullptr},
+    {"layernorm_bwd", (PyCFunction)(void *)guarded<layernorm_bwd, 10>, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
