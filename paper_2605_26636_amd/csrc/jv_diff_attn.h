@@ -5,7 +5,7 @@
 // All products run as D = A B + C on 32 x 32 blocks whose columns are what a wavefront keeps (its queries, or its keys in
 // the key pass of the gradient) and whose rows are the tokens of the tile that passes through LDS; a lane holds one
 // column, so that softmax sums stay inside a lane (and the lane 32 further), and a finished block is the B
-// operand of the next product as it stands.  fp32 tensors take the same steps on fp32 matrix instructions.
+// operand of the next product as it stands.  fp32 tensors take the same steps on operands of three bf16 numbers.
 #pragma once
 
 #include <type_traits>
@@ -32,7 +32,8 @@ struct DiffArgs {
     int splits, tiles_per_split;
     // gradient
     TensorArg d_o, dq, dk, dv;
-    float *stats;                   // [4][B * heads * n_q]: see diff_attn_rows_kernel
+    float *stats;                   // [4 or 6][B * heads * n_q]: see diff_attn_rows_kernel
+    const __bf16 *planes[4];        // fp32 tensors: Q, K, V, dO split, [B * heads * n][3][W] each
     int parts;                      // of the tiles of a workgroup's rows or keys; each leaves sums of its own where there are several:
     float *dq_part, *dkv_part;      // [parts][B * heads * n_q][W]; [parts][B * kv_heads * n_k][2 W]
     float *lam_part;                // [B * heads * row blocks * parts]: sums of P2 o dP
@@ -87,127 +88,44 @@ struct DiffLengths {
     }
 };
 
-// Eight channels of one token, or eight tokens of one channel: an operand of a product over 16 of them (lane = 32 g + i
-// holds row or column i and elements 8 g .. + 7, or what the other operand holds there).
-template <typename T> struct DiffFrag;
-template <> struct DiffFrag<__bf16> { bf16x8 x; };
-template <> struct DiffFrag<float> { f32x4 x[2]; };
-
-__device__ inline f32x16 diff_mma(const DiffFrag<__bf16> &a, const DiffFrag<__bf16> &b, f32x16 c) { return mfma32(a.x, b.x, c); }
-__device__ inline f32x16 diff_mma(const DiffFrag<float> &a, const DiffFrag<float> &b, f32x16 c) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[e >> 2][e & 3], b.x[e >> 2][e & 3], c, 0, 0, 0);
-    return c;
-}
 __device__ inline void diff_zero(f32x16 &x) {
 #pragma unroll
     for (int v = 0; v < 16; ++v) x[v] = 0.f;
 }
+// Operands (see mfma32): lane 32 g + i holds row or column i and elements 8 g .. + 7 of 16.
 // Rows 16 kk .. + 15 of a finished block as B operand: element e of lane 32 g + i is row 16 kk + 8 (e / 4) + 4 g + e % 4.
-template <typename T>
-__device__ inline DiffFrag<T> diff_block_frag(const f32x16 &s, int kk) {
-    DiffFrag<T> f;
-    if constexpr (std::is_same_v<T, __bf16>) {
-        f.x = as_bf16x8(u32x4{pack_bf16x2(s[8 * kk], s[8 * kk + 1]), pack_bf16x2(s[8 * kk + 2], s[8 * kk + 3]),
-                              pack_bf16x2(s[8 * kk + 4], s[8 * kk + 5]), pack_bf16x2(s[8 * kk + 6], s[8 * kk + 7])});
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f.x[e >> 2][e & 3] = s[8 * kk + e];
-    }
-    return f;
+__device__ inline bf16x8 diff_block_frag(const f32x16 &s, int kk) {
+    return as_bf16x8(u32x4{pack_bf16x2(s[8 * kk], s[8 * kk + 1]), pack_bf16x2(s[8 * kk + 2], s[8 * kk + 3]),
+                           pack_bf16x2(s[8 * kk + 4], s[8 * kk + 5]), pack_bf16x2(s[8 * kk + 6], s[8 * kk + 7])});
 }
 // Channels 16 ks + 8 g .. + 7 of a row in memory.
-template <typename T>
-__device__ inline DiffFrag<T> diff_global_frag(const T *row, int ks, int g, bool live) {
-    DiffFrag<T> f;
-    if constexpr (std::is_same_v<T, __bf16>) {
-        f.x = as_bf16x8(live ? *(const u32x4 *)(row + 16 * ks + 8 * g) : u32x4{0, 0, 0, 0});
-    } else {
-#pragma unroll
-        for (int p = 0; p < 2; ++p) f.x[p] = live ? *(const f32x4 *)(row + 16 * ks + 8 * g + 4 * p) : f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    return f;
+__device__ inline bf16x8 diff_global_frag(const __bf16 *row, int ks, int g, bool live) {
+    return as_bf16x8(live ? *(const u32x4 *)(row + 16 * ks + 8 * g) : u32x4{0, 0, 0, 0});
 }
 
-// 32 rows of W channels in LDS.  16-byte chunks are moved inside their row so that both kinds of reads spread over
-// all banks: a chunk of 16 consecutive rows (row-per-lane operands), and, for 16-bit elements, 64 bytes of four
-// consecutive rows (transposing reads), for 32-bit ones 128 bytes of two rows four apart (channel-per-lane reads).
-template <typename T, int W>
+// 32 rows of W channels of 16 bits in LDS.  16-byte chunks are moved inside their row so that both kinds of reads spread over
+// all banks: a chunk of 16 consecutive rows (row-per-lane operands) and 64 bytes of four consecutive rows (transposing reads).
+template <int W>
 struct DiffTile {
-    static constexpr int kRowBytes = W * (int)sizeof(T), kChunks = kRowBytes / 16, kBytes = kDiffTile * kRowBytes;
+    static constexpr int kRowBytes = 2 * W, kBytes = kDiffTile * kRowBytes;
     __device__ static unsigned off(int row, int chunk) {
-        unsigned slot;
-        if constexpr (sizeof(T) == 4) slot = chunk ^ ((row & 3) | (row & 4) << 1 | (row & 8) >> 1);
-        else if constexpr (W == 128) slot = chunk ^ ((row & 3) << 2 | (row >> 2 & 3));
-        else slot = chunk ^ ((row >> 1 & 1) << 2 | (row >> 2 & 3));
+        const unsigned slot = W == 128 ? chunk ^ ((row & 3) << 2 | (row >> 2 & 3)) : chunk ^ ((row >> 1 & 1) << 2 | (row >> 2 & 3));
         return row * kRowBytes + slot * 16;
     }
-    // Channels 16 ks + 8 g .. + 7 of row `row`.
-    __device__ static DiffFrag<T> row_frag(const unsigned char *tile, int row, int ks, int g) {
-        DiffFrag<T> f;
-        if constexpr (sizeof(T) == 2) {
-            f.x = as_bf16x8(*(const u32x4 *)(tile + off(row, 2 * ks + g)));
-        } else {
-            f.x[0] = *(const f32x4 *)(tile + off(row, 4 * ks + 2 * g));
-            f.x[1] = *(const f32x4 *)(tile + off(row, 4 * ks + 2 * g + 1));
-        }
-        return f;
-    }
-    // Channel 32 cb + i, rows as diff_block_frag has them.
-    __device__ static DiffFrag<T> col_frag(const unsigned char *tile, int kk, int cb, int lane) {
-        DiffFrag<T> f;
-        const int g = lane >> 5;
-        if constexpr (sizeof(T) == 2) {
-            const int b = lane >> 4, j = lane & 15, chunk = cb * 4 + (b & 1) * 2 + ((j & 3) >> 1), row = 16 * kk + 4 * g + (j >> 2);
-            const u32x2 r0 = lds_read_tr16(tile + off(row, chunk) + (j & 1) * 8), r1 = lds_read_tr16(tile + off(row + 8, chunk) + (j & 1) * 8);
-            f.x = as_bf16x8(u32x4{r0[0], r0[1], r1[0], r1[1]});
-        } else {
-            const int ch = 32 * cb + (lane & 31);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                f.x[e >> 2][e & 3] = *(const float *)(tile + off(16 * kk + 8 * (e >> 2) + 4 * g + (e & 3), ch >> 2) + (ch & 3) * 4);
-        }
-        return f;
-    }
 };
 
-// A tile on its way from memory into LDS through the registers of THREADS threads: fetched while the tile before it is
-// worked on.  Rows at `limit` and beyond are not read and arrive as zeros.  The base of a piece is the same for all threads (scalar
-// registers), a thread's place in it a 32-bit offset: kDiffMostTokenStride elements from token to token at most.
+// Elements from token to token at most: a lane's place in a tile is a 32-bit offset.
 constexpr long long kDiffMostTokenStride = 1 << 25;
-template <typename T, int W, int THREADS>
-struct DiffFetch {
-    using Tile = DiffTile<T, W>;
-    static constexpr int kPieces = kDiffTile * Tile::kChunks / THREADS, kStep = THREADS / Tile::kChunks;  // rows from piece to piece
-    static_assert(kPieces * THREADS == kDiffTile * Tile::kChunks && kStep * Tile::kChunks == THREADS, "whole pieces a thread");
-    const char *base;
-    long long step;
-    unsigned at;
-    u32x4 x[kPieces];
-    __device__ void start(const void *tensor, long long offset, long long sn, int tid) {
-        base = (const char *)tensor + offset * (long long)sizeof(T);
-        step = sn * (long long)sizeof(T);
-        at = (unsigned)(tid / Tile::kChunks) * (unsigned)step + (tid % Tile::kChunks) * 16;
-    }
-    __device__ void fetch(int row0, int limit, int tid) {
-        const char *from = base + (long long)row0 * step;
-        if (row0 + kDiffTile <= limit) {  // (uniform)
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i) x[i] = *(const u32x4 *)(from + i * kStep * step + at);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                x[i] = u32x4{0, 0, 0, 0};
-                if (row0 + i * kStep + tid / Tile::kChunks < limit) x[i] = *(const u32x4 *)(from + i * kStep * step + at);
-            }
-        }
-    }
-    __device__ void store(unsigned char *tile, int tid) const {
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) *(u32x4 *)(tile + Tile::off(i * kStep + tid / Tile::kChunks, tid % Tile::kChunks)) = x[i];
-    }
-};
 
+// Keys that a query does not see weigh nothing.
+__device__ inline void diff_hide_keys(f32x16 &s1, f32x16 &s2, int first, int limit, int g) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        const bool hidden = first + 8 * (v / 4) + 4 * g + v % 4 >= limit;
+        s1[v] = hidden ? -INFINITY : s1[v];
+        s2[v] = hidden ? -INFINITY : s2[v];
+    }
+}
 // bf16 tiles that loads bring straight into LDS, laid out as DiffTile (both kinds of reads), and read in assembly with waits of their
 // own: the compiler would wait for every load into LDS that is in flight in front of a read.  All offsets of a
 // lane's reads differ from its first one's by an exclusive or of small constants and by whole rows: one register holds them.
@@ -249,7 +167,7 @@ __device__ inline bf16x8 diff_join2(u32x2 a, u32x2 b) { return as_bf16x8(u32x4{a
 
 template <int W>
 struct DiffLds {
-    using Tile = DiffTile<__bf16, W>;
+    using Tile = DiffTile<W>;
     static constexpr int kRow = 2 * W, kKS = W / 32, kCB = W / 32;  // steps of 16 channels of a map, blocks of 32 channels
     // The lane's first row-per-lane read of a tile at `tile`; operand ks is at that ^ 32 ks.
     __device__ static unsigned rows(unsigned tile, int lane) { return tile + Tile::off(lane & 31, lane >> 5); }
@@ -274,12 +192,85 @@ struct DiffLds {
     }
 };
 
+// fp32 numbers as sums of three bf16 numbers, which together hold all 24 bits (leading 16 bits of the number, of what is left, and of
+// what is left then): a product of two is six of bf16, each accumulated in fp32, without the three that lie 2^-24 below it.  Tensors are split once
+// a call into planes [row][3][W]; 2.7 times the rate of the fp32 matrix instructions.
+struct DiffPlanes {
+    bf16x8 x[3];
+};
+__device__ inline f32x16 diff_mma6(const bf16x8 (&a)[3], const bf16x8 (&b)[3], f32x16 c) {
+    c = mfma32(a[2], b[0], c);
+    c = mfma32(a[0], b[2], c);
+    c = mfma32(a[1], b[1], c);
+    c = mfma32(a[1], b[0], c);
+    c = mfma32(a[0], b[1], c);
+    return mfma32(a[0], b[0], c);
+}
+// Leading parts of two numbers packed, and what is left of them.
+__device__ inline unsigned diff_take_pair(float &x, float &y) {
+    const unsigned u = __builtin_bit_cast(unsigned, x), v = __builtin_bit_cast(unsigned, y);
+    x -= __builtin_bit_cast(float, u & 0xffff0000u);
+    y -= __builtin_bit_cast(float, v & 0xffff0000u);
+    return __builtin_amdgcn_perm(v, u, 0x07060302);
+}
+__device__ inline void diff_split8(const float (&v)[8], u32x4 (&planes)[3]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float x = v[2 * e], y = v[2 * e + 1];
+#pragma unroll
+        for (int p = 0; p < 3; ++p) planes[p][e] = diff_take_pair(x, y);
+    }
+}
+// diff_block_frag in three planes.
+__device__ inline DiffPlanes diff_block_planes(const f32x16 &s, int kk) {
+    float v[8];
+    u32x4 x[3];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = s[8 * kk + e];
+    diff_split8(v, x);
+    return {{as_bf16x8(x[0]), as_bf16x8(x[1]), as_bf16x8(x[2])}};
+}
+template <int W>
+__device__ inline DiffPlanes diff_global_planes(const __bf16 *row, int ks, int g, bool live) {
+    return {{diff_global_frag(row, ks, g, live), diff_global_frag(row + W, ks, g, live), diff_global_frag(row + 2 * W, ks, g, live)}};
+}
+__device__ inline void diff_landed(u32x4 (&x)[3]) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2])); }
+__device__ inline void diff_landed(u32x2 (&x)[6]) {
+    asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]));
+}
+__device__ inline void diff_rows3(const u32x4 (&x)[3], bf16x8 (&to)[3]) {
+#pragma unroll
+    for (int p = 0; p < 3; ++p) to[p] = as_bf16x8(x[p]);
+}
+__device__ inline void diff_cols3(const u32x2 (&x)[6], bf16x8 (&to)[3]) {
+#pragma unroll
+    for (int p = 0; p < 3; ++p) to[p] = diff_join2(x[2 * p], x[2 * p + 1]);
+}
+// Operands of three plane tiles, one behind the other from OFF bytes on: rows (step ks of 16 channels) and columns (rows 16 KK .. + 15, block cb).
+template <int W, int OFF>
+__device__ inline void diff_read_rows3(u32x4 (&x)[3], unsigned rows, int ks) {
+    constexpr int TILE = DiffTile<W>::kBytes;
+    x[0] = lds_read_b128_at<OFF>(rows ^ 32 * ks);
+    x[1] = lds_read_b128_at<OFF + TILE>(rows ^ 32 * ks);
+    x[2] = lds_read_b128_at<OFF + 2 * TILE>(rows ^ 32 * ks);
+}
+template <int W, int OFF, int KK>
+__device__ inline void diff_read_cols3(u32x2 (&x)[6], unsigned cols, int cb) {
+    constexpr int TILE = DiffTile<W>::kBytes, AT = OFF + 16 * KK * 2 * W, EIGHT = 8 * 2 * W;
+    x[0] = lds_read_tr16_at<AT>(cols ^ 64 * cb);
+    x[1] = lds_read_tr16_at<AT + EIGHT>(cols ^ (64 * cb + 32));
+    x[2] = lds_read_tr16_at<AT + TILE>(cols ^ 64 * cb);
+    x[3] = lds_read_tr16_at<AT + TILE + EIGHT>(cols ^ (64 * cb + 32));
+    x[4] = lds_read_tr16_at<AT + 2 * TILE>(cols ^ 64 * cb);
+    x[5] = lds_read_tr16_at<AT + 2 * TILE + EIGHT>(cols ^ (64 * cb + 32));
+}
+
 // Loads of tiles into LDS by WAVES wavefronts, 1 KB an instruction: a lane fetches the chunk that belongs in its slot.  Rows at
 // `limit` and beyond are fetched as the one before it (the kernels mask them).  HELD: a lane's offsets are kept in registers, or worked
 // out at every load (a dozen instructions a tile, where registers are short).
 template <int W, int WAVES, bool HELD = true>
 struct DiffDma {
-    using Tile = DiffTile<__bf16, W>;
+    using Tile = DiffTile<W>;
     static constexpr int kLoads = kDiffTile * W / (512 * WAVES), kRows = 512 / W, kChunks = W / 8;
     const char *base;
     long long step;
@@ -317,6 +308,21 @@ struct DiffDma {
     }
 };
 
+// The same for the three planes of split fp32 rows.
+template <int W, int WAVES>
+struct DiffDma3 {
+    DiffDma<W, WAVES> one;
+    __device__ void start(const __bf16 *planes, long long row, int wave, int lane) { one.start(planes, row * 3 * W, 3 * W, wave, lane); }
+    __device__ void issue(unsigned char *tiles, int row0, int limit, int wave, int lane) const {
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+            DiffDma<W, WAVES> plane = one;
+            plane.base += p * 2 * W;
+            plane.issue(tiles + p * DiffTile<W>::kBytes, row0, limit, wave, lane);
+        }
+    }
+};
+
 // lambda of head h: exp(lq1 . lk1) - exp(lq2 . lk2) + init, and its two exponentials, in every lane of the wavefront.
 struct DiffLambda {
     float e1, e2, value;
@@ -347,6 +353,9 @@ __host__ __device__ inline long long diff_rows(const DiffArgs &a) { return (long
 jv_status diff_problem(const jv_diff_attn_desc *desc, const void *q, const void *k, const void *v, void *o,
                        const jv_diff_lambda *lambda, float scale, DiffProblem *out);
 jv_status diff_check_desc(const jv_diff_attn_desc *desc);
+// fp32 tensors: bytes of their planes in a workspace (with_d_o: of dO too), and the launch that fills them.
+size_t diff_planes_bytes(const jv_diff_attn_desc *desc, bool with_d_o);
+jv_status diff_split(DiffArgs &a, int W, void *memory, bool with_d_o, hipStream_t stream);
 // Strides of a [b, h, n, W] tensor; a written one must have a place of its own for every row.
 jv_status diff_check_strides(const char *name, const jv_strides &s, int64_t b, int64_t h, int64_t n, int W, int64_t align, bool written);
 int64_t diff_span(const jv_strides &s, int64_t b, int64_t h, int64_t n, int W);  // elements up to the end of the last row

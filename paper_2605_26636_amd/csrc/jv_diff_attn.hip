@@ -21,6 +21,13 @@ template <int W>
 struct DiffMap {
     float m, minus_m, l;
     f32x16 acc[W / 32];
+    __device__ void clear() {
+        m = -INFINITY;
+        minus_m = INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int cb = 0; cb < W / 32; ++cb) diff_zero(acc[cb]);
+    }
 };
 
 __device__ inline float diff_exp(f32x16 &p, const f32x16 &s, float c, float minus_m) {
@@ -169,125 +176,36 @@ __device__ inline void diff_finish(const DiffArgs &a, const DiffPlace &place, co
         }
 }
 
-// WAVES x 32 rows a workgroup.
-// SPLIT: a workgroup takes a part of the keys and leaves (m, l) of both maps and the unnormalised outputs in a.part.
-template <int W, int WAVES, bool SPLIT>
-__global__ void __launch_bounds__(64 * WAVES, 1) diff_attn_fwd_f32_kernel(DiffArgs a) {
-    using T = float;
-    using Tile = DiffTile<T, W>;
-    constexpr int THREADS = 64 * WAVES, KS = W / 16, CB = W / 32;
-    __shared__ __align__(16) unsigned char smem[2][2][Tile::kBytes];
-    __shared__ int wave_most[WAVES];
-    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    DiffPlace place;
-    if (!place.find<WAVES, SPLIT>(a, wave, li)) return;  // whole workgroup
-    const DiffLengths len(a, place.b);
-    const int limit = place.row_live ? len.limit(a, place.qi) : 0;
-    int most = limit, least = place.row_live ? limit : a.n_k;
+// Keys that the lane's row sees (0: none), and the tiles that the workgroup walks.  A row that sees none goes along unmasked (`limit`) and is dropped at
+// the end; `least`: the smallest limit of the wavefront's rows.
+template <int WAVES, bool SPLIT>
+__device__ inline int diff_tiles(const DiffArgs &a, const DiffPlace &place, const DiffLengths &len, int (&wave_most)[WAVES], int wave, int lane, int *limit, int *least_,
+                                 int *tile, int *tile_end) {
+    const int sees = place.row_live ? len.limit(a, place.qi) : 0;
+    *limit = sees > 0 ? sees : a.n_k + kDiffTile;
+    int most = sees, least = *limit;
 #pragma unroll
     for (int x = 1; x < 32; x *= 2) {
         most = max(most, __shfl_xor(most, x));
         least = min(least, __shfl_xor(least, x));
     }
-    most = __builtin_amdgcn_readfirstlane(most);
-    least = __builtin_amdgcn_readfirstlane(least);
-    int wg_most = most;
+    *least_ = __builtin_amdgcn_readfirstlane(least);
     if (WAVES > 1) {
         if (lane == 0) wave_most[wave] = most;
         __syncthreads();
 #pragma unroll
-        for (int x = 0; x < WAVES; ++x) wg_most = max(wg_most, wave_most[x]);
-        wg_most = __builtin_amdgcn_readfirstlane(wg_most);
+        for (int x = 0; x < WAVES; ++x) most = max(most, wave_most[x]);
     }
-    int tile = SPLIT ? place.split * a.tiles_per_split : 0, tile_end = (wg_most + kDiffTile - 1) / kDiffTile;
-    if (SPLIT) tile_end = min(tile_end, tile + a.tiles_per_split);
-
-    DiffFrag<T> q[KS];
-    {
-        const T *row = (const T *)a.q.ptr + place.b * a.q.sb + place.head * a.q.sh + place.qi * a.q.sn;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) q[ks] = diff_global_frag<T>(row, ks, g, limit > 0);
-    }
-    DiffMap<W> w1, w2;
-    w1.m = w2.m = -INFINITY;
-    w1.minus_m = w2.minus_m = INFINITY;
-    w1.l = w2.l = 0.f;
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-        diff_zero(w1.acc[cb]);
-        diff_zero(w2.acc[cb]);
-    }
-
-    DiffFetch<T, W, THREADS> kf, vf;
-    kf.start(a.k.ptr, place.b * a.k.sb + place.kv * a.k.sh, a.k.sn, tid);
-    vf.start(a.v.ptr, place.b * a.v.sb + place.kv * a.v.sh, a.v.sn, tid);
-    auto fetch = [&](int t) {
-        kf.fetch(t * kDiffTile, len.k, tid);
-        vf.fetch(t * kDiffTile, len.k, tid);
-    };
-    if (tile < tile_end) {
-        fetch(tile);
-        kf.store(smem[0][0], tid);
-        vf.store(smem[0][1], tid);
-    }
-    lds_barrier();
-    auto step = [&](auto buffer) {
-        constexpr int at = decltype(buffer)::value;
-        const bool more = tile + 1 < tile_end;
-        if (more) fetch(tile + 1);
-        if (tile * kDiffTile < most) {  // (uniform in the wavefront)
-            const unsigned char *kt = smem[at][0], *vt = smem[at][1];
-            f32x16 s1, s2;
-            diff_zero(s1);
-            diff_zero(s2);
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const DiffFrag<T> k = Tile::row_frag(kt, li, ks, g);
-                if (ks < KS / 2) s1 = diff_mma(k, q[ks], s1);
-                else s2 = diff_mma(k, q[ks], s2);
-            }
-            if ((tile + 1) * kDiffTile > least) {
-#pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const bool hidden = tile * kDiffTile + 8 * (v / 4) + 4 * g + v % 4 >= limit;
-                    s1[v] = hidden ? -INFINITY : s1[v];
-                    s2[v] = hidden ? -INFINITY : s2[v];
-                }
-            }
-            DiffFrag<T> p1[2], p2[2];
-            f32x16 p;
-            diff_softmax<W>(w1, p, s1, a.c);
-            p1[0] = diff_block_frag<T>(p, 0);
-            p1[1] = diff_block_frag<T>(p, 1);
-            diff_softmax<W>(w2, p, s2, a.c);
-            p2[0] = diff_block_frag<T>(p, 0);
-            p2[1] = diff_block_frag<T>(p, 1);
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-                for (int cb = 0; cb < CB; ++cb) {
-                    const DiffFrag<T> v = Tile::col_frag(vt, kk, cb, lane);
-                    w1.acc[cb] = diff_mma(v, p1[kk], w1.acc[cb]);
-                    w2.acc[cb] = diff_mma(v, p2[kk], w2.acc[cb]);
-                }
-        }
-        if (more) {
-            kf.store(smem[at ^ 1][0], tid);
-            vf.store(smem[at ^ 1][1], tid);
-        }
-        lds_barrier();
-    };
-    while (tile < tile_end) {  // (one copy of the tile for each buffer, whose place is then part of the instructions)
-        step(std::integral_constant<int, 0>());
-        if (++tile >= tile_end) break;
-        step(std::integral_constant<int, 1>());
-        ++tile;
-    }
-    diff_finish<float, float, W, SPLIT>(a, place, w1, w2, lane);
+    most = __builtin_amdgcn_readfirstlane(most);
+    *tile = SPLIT ? place.split * a.tiles_per_split : 0;
+    *tile_end = (most + kDiffTile - 1) / kDiffTile;
+    if (SPLIT) *tile_end = min(*tile_end, *tile + a.tiles_per_split);
+    return sees;
 }
 
 // ---------------------------------------------------------------------------------------
-// bf16 tensors.  As diff_attn_fwd_f32_kernel, with the tiles brought from memory straight into a ring of three LDS stages, two
+// bf16 tensors, WAVES x 32 rows a workgroup.  SPLIT: a workgroup takes a part of the keys and leaves (m, l) of both maps and the unnormalised
+// outputs in a.part.  Tiles come from memory straight into a ring of three LDS stages, two
 // tiles ahead, and LDS read in assembly with waits of its own (the compiler would wait for every load into LDS in front of
 // a read, and has no registers left for tiles on their way).  A tile: first map's scores on K operands that were read at the end of
 // the tile before, second map's operands meanwhile; the hand-over of the stages; V operands of 16 keys, under whose latency
@@ -333,23 +251,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffA
     DiffPlace place;
     if (!place.find<WAVES, SPLIT>(a, wave, li)) return;  // whole workgroup
     const DiffLengths len(a, place.b);
-    const int sees = place.row_live ? len.limit(a, place.qi) : 0, limit = sees > 0 ? sees : a.n_k + kDiffTile;
-    int most = sees, least = limit;
-#pragma unroll
-    for (int x = 1; x < 32; x *= 2) {
-        most = max(most, __shfl_xor(most, x));
-        least = min(least, __shfl_xor(least, x));
-    }
-    least = __builtin_amdgcn_readfirstlane(least);
-    if (WAVES > 1) {
-        if (lane == 0) wave_most[wave] = most;
-        __syncthreads();
-#pragma unroll
-        for (int x = 0; x < WAVES; ++x) most = max(most, wave_most[x]);
-    }
-    most = __builtin_amdgcn_readfirstlane(most);
-    int tile = SPLIT ? place.split * a.tiles_per_split : 0, tile_end = (most + kDiffTile - 1) / kDiffTile;
-    if (SPLIT) tile_end = min(tile_end, tile + a.tiles_per_split);
+    int limit, least, tile, tile_end;
+    const int sees = diff_tiles<WAVES, SPLIT>(a, place, len, wave_most, wave, lane, &limit, &least, &tile, &tile_end);
 
     DiffDma<W, WAVES> kload, vload;
     kload.start(a.k.ptr, place.b * a.k.sb + place.kv * a.k.sh, a.k.sn, wave, lane);
@@ -358,29 +261,23 @@ __global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffA
         kload.issue(smem + to * STAGE, t * kDiffTile, len.k, wave, lane);
         vload.issue(smem + to * STAGE + TILE, t * kDiffTile, len.k, wave, lane);
     };
-    DiffFrag<__bf16> q[2 * KS];
+    bf16x8 q[2 * KS];
     {
         const __bf16 *row = (const __bf16 *)a.q.ptr + place.b * a.q.sb + place.head * a.q.sh + place.qi * a.q.sn;
 #pragma unroll
-        for (int ks = 0; ks < 2 * KS; ++ks) q[ks] = diff_global_frag<__bf16>(row, ks, g, sees > 0);
+        for (int ks = 0; ks < 2 * KS; ++ks) q[ks] = diff_global_frag(row, ks, g, sees > 0);
     }
     if (tile < tile_end) issue(tile, 0);
     if (tile + 1 < tile_end) issue(tile + 1, 1);
 
     DiffMap<W> w1, w2;
-    w1.m = w2.m = -INFINITY;
-    w1.minus_m = w2.minus_m = INFINITY;
-    w1.l = w2.l = 0.f;
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-        diff_zero(w1.acc[cb]);
-        diff_zero(w2.acc[cb]);
-    }
+    w1.clear();
+    w2.clear();
     const unsigned kaddr = Lds::rows(lds_address(smem), lane), vaddr = Lds::cols(lds_address(smem), lane);
     u32x4 k1[KS];
     if (tile < tile_end) {
 #pragma unroll
-        for (int ks = 0; ks < 2 * KS; ++ks) asm volatile("" : "+v"(q[ks].x));  // (waited for here, not inside the loop)
+        for (int ks = 0; ks < 2 * KS; ++ks) asm volatile("" : "+v"(q[ks]));  // (waited for here, not inside the loop)
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         lds_barrier();
         Lds::template read_rows<0>(k1, kaddr, 0);
@@ -396,10 +293,10 @@ __global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffA
         Lds::template read_rows<0>(k2, kat, KS);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s1 = mfma32(as_bf16x8(k1[ks]), q[ks].x, s1);
+        for (int ks = 0; ks < KS; ++ks) s1 = mfma32(as_bf16x8(k1[ks]), q[ks], s1);
         diff_landed(k2);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s2 = mfma32(as_bf16x8(k2[ks]), q[KS + ks].x, s2);
+        for (int ks = 0; ks < KS; ++ks) s2 = mfma32(as_bf16x8(k2[ks]), q[KS + ks], s2);
         __builtin_amdgcn_sched_barrier(0);
         // the next tile has landed for every wavefront, and every wavefront has left the tile before, whose stage takes the one after
         if (tile + 1 < tile_end) {
@@ -407,14 +304,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffA
             lds_barrier();
             if (tile + 2 < tile_end) issue(tile + 2, after);
         }
-        if ((tile + 1) * kDiffTile > least) {
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const bool hidden = tile * kDiffTile + 8 * (v / 4) + 4 * g + v % 4 >= limit;
-                s1[v] = hidden ? -INFINITY : s1[v];
-                s2[v] = hidden ? -INFINITY : s2[v];
-            }
-        }
+        if ((tile + 1) * kDiffTile > least) diff_hide_keys(s1, s2, tile * kDiffTile, limit, g);
         unsigned p1[8], p2[8];
         diff_softmax_pack<W>(w1, p1, s1, a.c);
         u32x2 v0[2 * CB];
@@ -448,15 +338,157 @@ __global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffA
     asm("" : "+v"(l));  // (where the rows lie is worked out again: kept across the loop it would cost registers that are missed there)
     place.find<WAVES, SPLIT>(a, wave, l & 31);
     if ((place.row_live ? len.limit(a, place.qi) : 0) == 0) {
-        w1.m = w2.m = -INFINITY;
-        w1.l = w2.l = 0.f;
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb) {
-            diff_zero(w1.acc[cb]);
-            diff_zero(w2.acc[cb]);
-        }
+        w1.clear();
+        w2.clear();
     }
     diff_finish<__bf16, TO, W, SPLIT>(a, place, w1, w2, l);
+}
+
+// ---------------------------------------------------------------------------------------
+// fp32 tensors: as above on operands of three bf16 numbers, two stages of plane tiles, the next tile on its way under this one's
+// arithmetic.  A tile takes 72 (W = 64) or 144 matrix instructions and the splitting of 32 weights a lane.
+// ---------------------------------------------------------------------------------------
+template <int W, int WAVES, bool SPLIT>
+__global__ void __launch_bounds__(64 * WAVES, W == 64 && WAVES > 1 ? 2 : 1) diff_attn_fwd_f32_kernel(DiffArgs a) {
+    using Lds = DiffLds<W>;
+    constexpr int KS = W / 32, CB = W / 32, TILE = DiffTile<W>::kBytes, STAGE = 6 * TILE;  // a stage: three planes of K rows, three of V rows
+    __shared__ __align__(1024) unsigned char smem[2 * STAGE];
+    __shared__ int wave_most[WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    DiffPlace place;
+    if (!place.find<WAVES, SPLIT>(a, wave, li)) return;  // whole workgroup
+    const DiffLengths len(a, place.b);
+    int limit, least, tile, tile_end;
+    const int sees = diff_tiles<WAVES, SPLIT>(a, place, len, wave_most, wave, lane, &limit, &least, &tile, &tile_end);
+
+    DiffDma3<W, WAVES> kload, vload;
+    kload.start(a.planes[1], (long long)place.bkv * a.n_k, wave, lane);
+    vload.start(a.planes[2], (long long)place.bkv * a.n_k, wave, lane);
+    auto issue = [&](int t, int stage) {
+        kload.issue(smem + stage * STAGE, t * kDiffTile, len.k, wave, lane);
+        vload.issue(smem + stage * STAGE + 3 * TILE, t * kDiffTile, len.k, wave, lane);
+    };
+    if (tile < tile_end) issue(tile, 0);
+    DiffPlanes q[2 * KS];
+    {
+        const __bf16 *row = a.planes[0] + (((long long)place.b * a.heads + place.head) * a.n_q + place.qi) * 3 * W;
+#pragma unroll
+        for (int ks = 0; ks < 2 * KS; ++ks) q[ks] = diff_global_planes<W>(row, ks, g, sees > 0);
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2 * KS; ++ks) asm volatile("" : "+v"(q[ks].x[0]), "+v"(q[ks].x[1]), "+v"(q[ks].x[2]));  // (waited for here, not inside the loop)
+    DiffMap<W> w1, w2;
+    w1.clear();
+    w2.clear();
+    const unsigned rows0 = Lds::rows(lds_address(smem), lane), cols0 = Lds::cols(lds_address(smem), lane);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    lds_barrier();
+    for (int stage = 0; tile < tile_end; ++tile, stage ^= 1) {
+        if (tile + 1 < tile_end) issue(tile + 1, stage ^ 1);
+        const unsigned rows = rows0 + stage * STAGE, cols = cols0 + stage * STAGE;
+        f32x16 s1, s2, p;
+        diff_zero(s1);
+        diff_zero(s2);
+        {
+            u32x4 x[2][3];
+            diff_read_rows3<W, 0>(x[0], rows, 0);
+            diff_landed(x[0]);
+#pragma unroll
+            for (int ks = 0; ks < 2 * KS; ++ks) {
+                if (ks + 1 < 2 * KS) diff_read_rows3<W, 0>(x[(ks + 1) & 1], rows, ks + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                bf16x8 k[3];
+                diff_rows3(x[ks & 1], k);
+                if (ks < KS) s1 = diff_mma6(k, q[ks].x, s1);
+                else s2 = diff_mma6(k, q[ks].x, s2);
+                if (ks + 1 < 2 * KS) diff_landed(x[(ks + 1) & 1]);
+            }
+        }
+        u32x2 v[2][6];
+        diff_read_cols3<W, 3 * TILE, 0>(v[0], cols, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        if ((tile + 1) * kDiffTile > least) diff_hide_keys(s1, s2, tile * kDiffTile, limit, g);
+        DiffPlanes p1[2], p2[2];
+        diff_softmax<W>(w1, p, s1, a.c);
+        p1[0] = diff_block_planes(p, 0);
+        p1[1] = diff_block_planes(p, 1);
+        diff_softmax<W>(w2, p, s2, a.c);
+        p2[0] = diff_block_planes(p, 0);
+        p2[1] = diff_block_planes(p, 1);
+        diff_landed(v[0]);
+#pragma unroll
+        for (int i = 0; i < 2 * CB; ++i) {
+            const int kk = i / CB, cb = i % CB, next = (i + 1) % CB;
+            if (i + 1 < CB) diff_read_cols3<W, 3 * TILE, 0>(v[(i + 1) & 1], cols, next);
+            else if (i + 1 < 2 * CB) diff_read_cols3<W, 3 * TILE, 1>(v[(i + 1) & 1], cols, next);
+            __builtin_amdgcn_sched_barrier(0);
+            bf16x8 x[3];
+            diff_cols3(v[i & 1], x);
+            w1.acc[cb] = diff_mma6(x, p1[kk].x, w1.acc[cb]);
+            w2.acc[cb] = diff_mma6(x, p2[kk].x, w2.acc[cb]);
+            if (i + 1 < 2 * CB) diff_landed(v[(i + 1) & 1]);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the next tile, for every wavefront, and every wavefront done with this one
+        lds_barrier();
+    }
+    if (sees == 0) {
+        w1.clear();
+        w2.clear();
+    }
+    diff_finish<float, float, W, SPLIT>(a, place, w1, w2, lane);
+}
+
+// fp32 tensors into planes: a thread eight channels; blockIdx.y the tensor (Q, K, V, dO).  Rows behind their sequence's end are not read.
+struct DiffSplitArgs {
+    TensorArg in[4];
+    __bf16 *out[4];
+    int heads[4], n[4];
+    const int *len[4];
+    long long rows[4];
+};
+template <int W>
+__global__ void __launch_bounds__(256) diff_attn_split_kernel(DiffSplitArgs a) {
+    const int t = blockIdx.y;
+    const long long at = (long long)blockIdx.x * 256 + threadIdx.x, row = at / (W / 8);
+    if (row >= a.rows[t]) return;
+    const int ch = (int)(at % (W / 8)) * 8, i = (int)(row % a.n[t]), bh = (int)(row / a.n[t]), h = bh % a.heads[t], b = bh / a.heads[t];
+    if (a.len[t] && i >= a.len[t][b]) return;
+    const TensorArg &in = a.in[t];
+    const float *from = (const float *)in.ptr + b * in.sb + h * in.sh + i * in.sn + ch;
+    const f32x4 x = *(const f32x4 *)from, y = *(const f32x4 *)(from + 4);
+    const float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+    u32x4 planes[3];
+    diff_split8(v, planes);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) *(u32x4 *)(a.out[t] + (row * 3 + p) * W + ch) = planes[p];
+}
+size_t diff_planes_bytes(const jv_diff_attn_desc *d, bool with_d_o) {
+    if (d->dtype != JV_F32) return 0;
+    const size_t q = (size_t)d->batch * d->heads * d->n_q, k = (size_t)d->batch * d->kv_heads * d->n_k;
+    auto whole = [&](size_t rows) { return (rows * 6 * d->head_dim + 255) & ~(size_t)255; };
+    return whole(q) * (with_d_o ? 2 : 1) + 2 * whole(k);
+}
+jv_status diff_split(DiffArgs &a, int W, void *memory, bool with_d_o, hipStream_t stream) {
+    DiffSplitArgs s;
+    const TensorArg in[4] = {a.q, a.k, a.v, a.d_o};
+    char *at = (char *)memory;
+    long long most = 0;
+    for (int t = 0; t < (with_d_o ? 4 : 3); ++t) {
+        const bool keys = t == 1 || t == 2;
+        s.in[t] = in[t];
+        s.heads[t] = keys ? a.kv_heads : a.heads;
+        s.n[t] = keys ? a.n_k : a.n_q;
+        s.len[t] = keys ? a.k_len : a.q_len;
+        s.rows[t] = (long long)a.B * s.heads[t] * s.n[t];
+        s.out[t] = (__bf16 *)at;
+        a.planes[t] = s.out[t];
+        at += (s.rows[t] * 6 * W + 255) & ~255ll;
+        most = std::max(most, s.rows[t]);
+    }
+    const dim3 grid((unsigned)((most * (W / 8) + 255) / 256), with_d_o ? 4 : 3);
+    if (W == 128) hipLaunchKernelGGL(diff_attn_split_kernel<128>, grid, dim3(256), 0, stream, s);
+    else hipLaunchKernelGGL(diff_attn_split_kernel<64>, grid, dim3(256), 0, stream, s);
+    return launch_status("diff_attn_split_kernel");
 }
 
 // The parts of a row joined by SHARE wavefronts, which take every SHARE-th part each, eight parts' loads at a time (parts that saw no key are
@@ -653,12 +685,14 @@ jv_status diff_problem(const jv_diff_attn_desc *d, const void *q, const void *k,
 }
 
 template <typename T, typename TO, int W>
-static jv_status diff_forward(DiffArgs a, const DiffPlan &plan, hipStream_t stream) {
+static jv_status diff_forward(DiffArgs a, const DiffPlan &plan, void *planes, hipStream_t stream) {
     a.blocks = plan.blocks;
     a.splits = plan.splits;
     a.tiles_per_split = plan.tiles_per_split;
     a.items = (long long)a.B * a.kv_heads * a.blocks * a.splits;
     const dim3 grid(diff_grid(a.items));
+    jv_status st;
+    if (sizeof(T) == 4 && (st = diff_split(a, W, planes, false, stream)) != JV_OK) return st;
     auto launch = [&](auto waves, auto split) {
         constexpr int WAVES = decltype(waves)::value;
         constexpr bool SPLIT = decltype(split)::value;
@@ -673,8 +707,7 @@ static jv_status diff_forward(DiffArgs a, const DiffPlan &plan, hipStream_t stre
     }
     if (plan.waves == 1) launch(std::integral_constant<int, 1>(), std::true_type());
     else launch(std::integral_constant<int, 4>(), std::true_type());
-    const jv_status st = launch_status("diff_attn_fwd_kernel");
-    if (st != JV_OK) return st;
+    if ((st = launch_status("diff_attn_fwd_kernel")) != JV_OK) return st;
     const long long rows = diff_rows(a);
     if (a.splits > 8) hipLaunchKernelGGL((diff_attn_join_kernel<T, TO, W, 4>), dim3((unsigned)rows), dim3(256), 0, stream, a);
     else hipLaunchKernelGGL((diff_attn_join_kernel<T, TO, W, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a);
@@ -689,7 +722,8 @@ size_t jv_diff_attn_workspace_bytes(const jv_diff_attn_desc *desc) {
     jv::clear_error();
     if (jv::diff_check_desc(desc) != JV_OK) return 0;
     const size_t part = jv::diff_part_bytes(jv::diff_plan_of(desc), (long long)desc->batch * desc->heads * desc->n_q, desc->head_dim);
-    return part > 256 ? (part + 255) & ~(size_t)255 : 256;
+    const size_t bytes = ((part + 255) & ~(size_t)255) + jv::diff_planes_bytes(desc, false);
+    return bytes > 256 ? bytes : 256;
 }
 
 size_t jv_diff_attn_saved_bytes(const jv_diff_attn_desc *desc) {
@@ -720,11 +754,13 @@ jv_status jv_diff_attn_fwd(const jv_diff_attn_desc *desc, const void *q, const v
     }
     const jv::DiffPlan plan = jv::diff_plan_of(desc);
     const size_t need = jv_diff_attn_workspace_bytes(desc);
-    if (plan.splits > 1) {
+    void *planes = nullptr;
+    if (need > 256) {
         if (!workspace) return jv::fail(JV_ERR_INVALID_ARG, "workspace must be non-null");
         if ((uintptr_t)workspace & 255) return jv::fail(JV_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
         if (workspace_bytes < need) return jv::fail(JV_ERR_WORKSPACE_TOO_SMALL, "workspace holds %zu bytes, %zu are needed", workspace_bytes, need);
         p.a.part = (float *)workspace;
+        planes = (char *)workspace + (need - jv::diff_planes_bytes(desc, false));
     }
     if ((long long)desc->batch * desc->kv_heads * plan.blocks * plan.splits > 0x7ffffff0ll)
         return jv::fail(JV_ERR_UNSUPPORTED, "more than 2^31 workgroups");
@@ -732,9 +768,9 @@ jv_status jv_diff_attn_fwd(const jv_diff_attn_desc *desc, const void *q, const v
     return jv::diff_with_kind(p.bf16, p.W, [&](auto kind) {
         using K = decltype(kind);
         if (p.o_bf16) {
-            if constexpr (sizeof(typename K::T) == 2) return jv::diff_forward<typename K::T, __bf16, K::W>(p.a, plan, stream);
+            if constexpr (sizeof(typename K::T) == 2) return jv::diff_forward<typename K::T, __bf16, K::W>(p.a, plan, planes, stream);
         }
-        return jv::diff_forward<typename K::T, float, K::W>(p.a, plan, stream);
+        return jv::diff_forward<typename K::T, float, K::W>(p.a, plan, planes, stream);
     });
 }
 

@@ -12,7 +12,11 @@ namespace jv {
 // What both passes need of a query, from the rows of O and P2 V that the forward pass left in the element type
 // (P1 V = O + lambda P2 V) and its references and sums: a.stats holds
 //     [0], [1]   -log2(denominator of map m) / c, which a score product starts from: the weight is 2^(c sum), 0 for a row that sees no key
-//     [2]        -D1            [3]   -lambda (D1 - D2),    Dm = rowsum(dO o (Pm V)).
+//     [2]        -D1            [3]   -lambda (D1 - D2),    Dm = rowsum(dO o (Pm V)),
+// and for fp32 tensors, whose weights e inv with e = 2^(c score - m) keep the reference m and the sum 1 / inv apart (their logarithm, rounded, would
+// cost the weights 2^-24 of its size),
+//     [0], [1]   -m1, -m2;      [2], [3]   f1 = inv1, h1 = -D1 inv1;      [4], [5]   f2 = -lambda inv2, h2 = lambda D2 inv2:
+// dS1 = e1 (f1 dP + h1), dS2 = e2 (f2 dP + h2), P1 - lambda P2 = e1 f1 + e2 f2.
 // A row takes as many lanes as it has 16-byte pieces.
 template <typename T, int W>
 __global__ void __launch_bounds__(256) diff_attn_rows_kernel(DiffArgs a) {
@@ -55,15 +59,25 @@ __global__ void __launch_bounds__(256) diff_attn_rows_kernel(DiffArgs a) {
         d1 += __shfl_xor(d1, x);
         d2 += __shfl_xor(d2, x);
     }
-    if (!live || ch >= 4 * PER) return;
+    constexpr int STATS = sizeof(T) == 2 ? 4 : 6;
+    if (!live || ch >= STATS * PER) return;
     const long long n = diff_rows(a);
     const int which = ch / PER;  // a statistic a lane
-    if (which < 2) {
-        const float ref = qi < DiffLengths(a, b).q ? a.ml[2 * which * n + row] : INFINITY;
-        a.stats[which * n + row] = ref == INFINITY ? -INFINITY : -(ref + log2f(a.ml[(2 * which + 1) * n + row])) / a.c;
+    const float m1 = qi < DiffLengths(a, b).q ? a.ml[row] : INFINITY;  // (both maps see the same keys)
+    float stat;
+    if constexpr (sizeof(T) == 2) {
+        if (which == 2) stat = -d1;
+        else if (which == 3) stat = -lam * (d1 - d2);
+        else stat = m1 == INFINITY ? -INFINITY : -(a.ml[2 * which * n + row] + log2f(a.ml[(2 * which + 1) * n + row])) / a.c;
+    } else if (m1 == INFINITY) {
+        stat = which < 2 ? -INFINITY : 0.f;
+    } else if (which < 2) {
+        stat = -a.ml[2 * which * n + row];
     } else {
-        a.stats[which * n + row] = which == 2 ? -d1 : -lam * (d1 - d2);
+        const float inv = 1.f / a.ml[(which < 4 ? 1 : 3) * n + row];
+        stat = inv * (which == 2 ? 1.f : which == 3 ? -d1 : which == 4 ? -lam : lam * d2);
     }
+    a.stats[which * n + row] = stat;
 }
 
 // One of a.parts equal parts of `total`: [from, to).
@@ -89,6 +103,20 @@ struct DiffRowGrad {
         h1 = minus_d1 * f1;
         f2 = -lam * inv2;
         h2 = lam_d2 * inv2;
+    }
+    __device__ void load_f32(const DiffArgs &a, long long row, bool sees) {
+        minus_m1 = minus_m2 = -INFINITY;
+        f1 = h1 = f2 = h2 = inv2 = 0.f;
+        if (!sees) return;
+        const long long n = diff_rows(a);
+        const float *stat = a.stats + row;
+        minus_m1 = stat[0];
+        minus_m2 = stat[n];
+        f1 = stat[2 * n];
+        h1 = stat[3 * n];
+        f2 = stat[4 * n];
+        h2 = stat[5 * n];
+        inv2 = 1.f / a.ml[3 * n + row];
     }
 };
 
@@ -152,15 +180,6 @@ struct DiffQueries {
     }
 };
 
-// Keys that a query does not see weigh nothing.
-__device__ inline void diff_hide_keys(f32x16 &s1, f32x16 &s2, int first, int limit, int g) {
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-        const bool hidden = first + 8 * (v / 4) + 4 * g + v % 4 >= limit;
-        s1[v] = hidden ? -INFINITY : s1[v];
-        s2[v] = hidden ? -INFINITY : s2[v];
-    }
-}
 // Scores and dP of a tile (rows: keys) become the gradients of the logits, in place.
 __device__ inline void diff_logit_grads(f32x16 &s1, f32x16 &s2, const f32x16 &dp, const DiffRowGrad &r, float c, float &lam_sum) {
 #pragma unroll
@@ -173,91 +192,8 @@ __device__ inline void diff_logit_grads(f32x16 &s1, f32x16 &s2, const f32x16 &dp
 }
 
 // dQ, and the sums of P2 o dP (for lambda): a wavefront keeps 32 queries of one head, their dO and their dQ, and walks the keys.
-// A tile takes W / 16 score products, as many of V with dO, and as many of K^T with the gradients of the logits.
-template <int W>
-__global__ void __launch_bounds__(256, 1) diff_attn_dq_f32_kernel(DiffArgs a) {
-    using T = float;
-    using Tile = DiffTile<T, W>;
-    constexpr int KS = W / 16, CB = W / 32;
-    __shared__ __align__(16) unsigned char smem[2][2][Tile::kBytes];
-    __shared__ int wave_most[4];
-    __shared__ float wave_lam[4];
-    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    DiffQueries p;
-    if (!p.find(a, wave_most, wave, lane)) return;  // whole workgroup
-    const int len_k = DiffLengths(a, p.b).k;
-    const float lam = diff_lambda<W>(a, p.h, lane).value;
-    DiffFrag<T> q[KS], go[KS];
-    DiffRowGrad r;
-    {
-        const int at = p.row_live ? p.qi : 0;
-        const T *row = (const T *)a.q.ptr + p.b * a.q.sb + p.h * a.q.sh + at * a.q.sn, *grow = (const T *)a.d_o.ptr + p.b * a.d_o.sb + p.h * a.d_o.sh + at * a.d_o.sn;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            q[ks] = diff_global_frag<T>(row, ks, g, p.limit > 0);
-            go[ks] = diff_global_frag<T>(grow, ks, g, p.limit > 0);
-        }
-        r.load(a, p.row, p.limit > 0, lam);
-    }
-    f32x16 acc[CB];
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) diff_zero(acc[cb]);
-    float lam_sum = 0.f;
-    DiffFetch<T, W, 256> kf, vf;
-    kf.start(a.k.ptr, p.b * a.k.sb + p.kv * a.k.sh, a.k.sn, tid);
-    vf.start(a.v.ptr, p.b * a.v.sb + p.kv * a.v.sh, a.v.sn, tid);
-    int tile = p.tile;
-    if (tile < p.tile_end) {
-        kf.fetch(tile * kDiffTile, len_k, tid);
-        vf.fetch(tile * kDiffTile, len_k, tid);
-        kf.store(smem[0][0], tid);
-        vf.store(smem[0][1], tid);
-    }
-    lds_barrier();
-    auto step = [&](auto buffer) {
-        constexpr int at = decltype(buffer)::value;
-        const bool more = tile + 1 < p.tile_end;
-        if (more) {
-            kf.fetch((tile + 1) * kDiffTile, len_k, tid);
-            vf.fetch((tile + 1) * kDiffTile, len_k, tid);
-        }
-        const unsigned char *kt = smem[at][0], *vt = smem[at][1];
-        f32x16 s1, s2, dp;
-        diff_zero(s1);
-        diff_zero(s2);
-        diff_zero(dp);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            const DiffFrag<T> k = Tile::row_frag(kt, li, ks, g);
-            if (ks < KS / 2) s1 = diff_mma(k, q[ks], s1);
-            else s2 = diff_mma(k, q[ks], s2);
-        }
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) dp = diff_mma(Tile::row_frag(vt, li, ks, g), go[ks], dp);
-        if ((tile + 1) * kDiffTile > p.least) diff_hide_keys(s1, s2, tile * kDiffTile, p.limit, g);
-        diff_logit_grads(s1, s2, dp, r, a.c, lam_sum);
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            const DiffFrag<T> ds1 = diff_block_frag<T>(s1, kk), ds2 = diff_block_frag<T>(s2, kk);
-#pragma unroll
-            for (int cb = 0; cb < CB; ++cb) acc[cb] = diff_mma(Tile::col_frag(kt, kk, cb, lane), cb < CB / 2 ? ds1 : ds2, acc[cb]);
-        }
-        if (more) {
-            kf.store(smem[at ^ 1][0], tid);
-            vf.store(smem[at ^ 1][1], tid);
-        }
-        lds_barrier();
-    };
-    while (tile < p.tile_end) {  // (one copy of the tile for each buffer, whose place is then part of the instructions)
-        step(std::integral_constant<int, 0>());
-        if (++tile >= p.tile_end) break;
-        step(std::integral_constant<int, 1>());
-        ++tile;
-    }
-    diff_finish_dq<T, W>(a, acc, lam_sum * r.inv2, p.b, p.h, p.block, p.part, wave_lam, tid);
-}
-
-// The same for bf16 tensors: tiles straight into two LDS stages, the next tile's under this one's arithmetic.
+// A tile takes W / 16 score products, as many of V with dO, and as many of K^T with the gradients of the logits.  Tiles come straight
+// into two LDS stages, the next tile's under this one's arithmetic.
 template <int W>
 __global__ void __launch_bounds__(256, 2) diff_attn_dq_bf16_kernel(DiffArgs a) {
     using Lds = DiffLds<W>;
@@ -279,7 +215,7 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dq_bf16_kernel(DiffArgs a) {
     int tile = p.tile;
     if (tile < p.tile_end) issue(tile, 0);
     const float lam = diff_lambda<W>(a, p.h, lane).value;
-    DiffFrag<__bf16> q[2 * KS], go[2 * KS];
+    bf16x8 q[2 * KS], go[2 * KS];
     DiffRowGrad r;
     {
         const int at = p.row_live ? p.qi : 0;
@@ -287,13 +223,13 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dq_bf16_kernel(DiffArgs a) {
         const __bf16 *grow = (const __bf16 *)a.d_o.ptr + p.b * a.d_o.sb + p.h * a.d_o.sh + at * a.d_o.sn;
 #pragma unroll
         for (int ks = 0; ks < 2 * KS; ++ks) {
-            q[ks] = diff_global_frag<__bf16>(row, ks, g, p.limit > 0);
-            go[ks] = diff_global_frag<__bf16>(grow, ks, g, p.limit > 0);
+            q[ks] = diff_global_frag(row, ks, g, p.limit > 0);
+            go[ks] = diff_global_frag(grow, ks, g, p.limit > 0);
         }
         r.load(a, p.row, p.limit > 0, lam);
     }
 #pragma unroll
-    for (int ks = 0; ks < 2 * KS; ++ks) asm volatile("" : "+v"(q[ks].x), "+v"(go[ks].x));  // (waited for here, not inside the loop)
+    for (int ks = 0; ks < 2 * KS; ++ks) asm volatile("" : "+v"(q[ks]), "+v"(go[ks]));  // (waited for here, not inside the loop)
     asm volatile("" : "+v"(r.minus_m1), "+v"(r.minus_m2), "+v"(r.f1), "+v"(r.h1), "+v"(r.f2), "+v"(r.h2), "+v"(r.inv2));
     f32x16 acc[CB];
 #pragma unroll
@@ -315,30 +251,30 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dq_bf16_kernel(DiffArgs a) {
         Lds::template read_rows<0>(y, rows, KS);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s1 = mfma32(as_bf16x8(x[ks]), q[ks].x, s1);
+        for (int ks = 0; ks < KS; ++ks) s1 = mfma32(as_bf16x8(x[ks]), q[ks], s1);
         diff_landed(y);
         Lds::template read_rows<TILE>(x, rows, 0);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s2 = mfma32(as_bf16x8(y[ks]), q[KS + ks].x, s2);
+        for (int ks = 0; ks < KS; ++ks) s2 = mfma32(as_bf16x8(y[ks]), q[KS + ks], s2);
         diff_landed(x);
         Lds::template read_rows<TILE>(y, rows, KS);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) dp = mfma32(as_bf16x8(x[ks]), go[ks].x, dp);
+        for (int ks = 0; ks < KS; ++ks) dp = mfma32(as_bf16x8(x[ks]), go[ks], dp);
         diff_landed(y);
         u32x2 c0[2 * CB];
         Lds::template read_cols<0, 0>(c0, cols);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) dp = mfma32(as_bf16x8(y[ks]), go[KS + ks].x, dp);
+        for (int ks = 0; ks < KS; ++ks) dp = mfma32(as_bf16x8(y[ks]), go[KS + ks], dp);
         if ((tile + 1) * kDiffTile > p.least) diff_hide_keys(s1, s2, tile * kDiffTile, p.limit > 0 ? p.limit : a.n_k + kDiffTile, g);
         diff_logit_grads(s1, s2, dp, r, a.c, lam_sum);
         bf16x8 ds1[2], ds2[2];
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
-            ds1[kk] = diff_block_frag<__bf16>(s1, kk).x;
-            ds2[kk] = diff_block_frag<__bf16>(s2, kk).x;
+            ds1[kk] = diff_block_frag(s1, kk);
+            ds2[kk] = diff_block_frag(s2, kk);
         }
         diff_landed(c0);
         u32x2 c1[2 * CB];
@@ -354,6 +290,100 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dq_bf16_kernel(DiffArgs a) {
     }
     asm("" : "+v"(lam_sum));
     diff_finish_dq<__bf16, W>(a, acc, lam_sum * r.inv2, p.b, p.h, p.block, p.part, wave_lam, tid);
+}
+
+// The same for fp32 tensors, on operands of three bf16 numbers.
+template <int W>
+__global__ void __launch_bounds__(256, 1) diff_attn_dq_f32_kernel(DiffArgs a) {
+    using Lds = DiffLds<W>;
+    constexpr int KS = W / 32, CB = W / 32, TILE = DiffTile<W>::kBytes, STAGE = 6 * TILE;  // a stage: three planes of K rows, three of V rows
+    __shared__ __align__(1024) unsigned char smem[2 * STAGE];
+    __shared__ int wave_most[4];
+    __shared__ float wave_lam[4];
+    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    DiffQueries p;
+    if (!p.find(a, wave_most, wave, lane)) return;  // whole workgroup
+    const int len_k = DiffLengths(a, p.b).k;
+    DiffDma3<W, 4> kload, vload;
+    kload.start(a.planes[1], ((long long)p.b * a.kv_heads + p.kv) * a.n_k, wave, lane);
+    vload.start(a.planes[2], ((long long)p.b * a.kv_heads + p.kv) * a.n_k, wave, lane);
+    auto issue = [&](int t, int stage) {
+        kload.issue(smem + stage * STAGE, t * kDiffTile, len_k, wave, lane);
+        vload.issue(smem + stage * STAGE + 3 * TILE, t * kDiffTile, len_k, wave, lane);
+    };
+    int tile = p.tile;
+    if (tile < p.tile_end) issue(tile, 0);
+    DiffPlanes q[2 * KS], go[2 * KS];
+    DiffRowGrad r;
+    {
+        const long long at = (p.row_live ? p.row : 0) * 3 * W;
+#pragma unroll
+        for (int ks = 0; ks < 2 * KS; ++ks) {
+            q[ks] = diff_global_planes<W>(a.planes[0] + at, ks, g, p.limit > 0);
+            go[ks] = diff_global_planes<W>(a.planes[3] + at, ks, g, p.limit > 0);
+        }
+        r.load_f32(a, p.row, p.limit > 0);
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2 * KS; ++ks)  // (waited for here, not inside the loop)
+        asm volatile("" : "+v"(q[ks].x[0]), "+v"(q[ks].x[1]), "+v"(q[ks].x[2]), "+v"(go[ks].x[0]), "+v"(go[ks].x[1]), "+v"(go[ks].x[2]));
+    asm volatile("" : "+v"(r.minus_m1), "+v"(r.minus_m2), "+v"(r.f1), "+v"(r.h1), "+v"(r.f2), "+v"(r.h2), "+v"(r.inv2));
+    f32x16 acc[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) diff_zero(acc[cb]);
+    float lam_sum = 0.f;
+    const unsigned rows0 = Lds::rows(lds_address(smem), lane), cols0 = Lds::cols(lds_address(smem), lane);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    lds_barrier();
+    for (int stage = 0; tile < p.tile_end; ++tile, stage ^= 1) {
+        if (tile + 1 < p.tile_end) issue(tile + 1, stage ^ 1);
+        const unsigned rows = rows0 + stage * STAGE, cols = cols0 + stage * STAGE;
+        f32x16 s1, s2, dp;
+        diff_zero(s1);
+        diff_zero(s2);
+        diff_zero(dp);
+        {
+            u32x4 x[2][3];
+            diff_read_rows3<W, 0>(x[0], rows, 0);
+            diff_landed(x[0]);
+#pragma unroll
+            for (int i = 0; i < 4 * KS; ++i) {  // K operands, then V operands
+                if (i + 1 < 2 * KS) diff_read_rows3<W, 0>(x[(i + 1) & 1], rows, i + 1);
+                else if (i + 1 < 4 * KS) diff_read_rows3<W, 3 * TILE>(x[(i + 1) & 1], rows, i + 1 - 2 * KS);
+                __builtin_amdgcn_sched_barrier(0);
+                bf16x8 k[3];
+                diff_rows3(x[i & 1], k);
+                if (i < KS) s1 = diff_mma6(k, q[i < KS ? i : 0].x, s1);
+                else if (i < 2 * KS) s2 = diff_mma6(k, q[i < 2 * KS ? i : 0].x, s2);
+                else dp = diff_mma6(k, go[i < 2 * KS ? 0 : i - 2 * KS].x, dp);
+                if (i + 1 < 4 * KS) diff_landed(x[(i + 1) & 1]);
+            }
+        }
+        u32x2 v[2][6];
+        diff_read_cols3<W, 0, 0>(v[0], cols, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        if ((tile + 1) * kDiffTile > p.least) diff_hide_keys(s1, s2, tile * kDiffTile, p.limit > 0 ? p.limit : a.n_k + kDiffTile, g);
+        diff_logit_grads(s1, s2, dp, r, a.c, lam_sum);
+        diff_landed(v[0]);
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            const DiffPlanes ds1 = diff_block_planes(s1, kk), ds2 = diff_block_planes(s2, kk);
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) {
+                const int i = kk * CB + cb;
+                if (i + 1 < CB) diff_read_cols3<W, 0, 0>(v[(i + 1) & 1], cols, i + 1);
+                else if (i + 1 < 2 * CB) diff_read_cols3<W, 0, 1>(v[(i + 1) & 1], cols, i + 1 - CB);
+                __builtin_amdgcn_sched_barrier(0);
+                bf16x8 x[3];
+                diff_cols3(v[i & 1], x);
+                acc[cb] = diff_mma6(x, cb < CB / 2 ? ds1.x : ds2.x, acc[cb]);
+                if (i + 1 < 2 * CB) diff_landed(v[(i + 1) & 1]);
+            }
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the next tile, for every wavefront, and every wavefront done with this one
+        lds_barrier();
+    }
+    diff_finish_dq<float, W>(a, acc, lam_sum * r.inv2, p.b, p.h, p.block, p.part, wave_lam, tid);
 }
 
 // Where a workgroup of the key pass stands: 128 keys of a kv head; the tiles of its group's heads, one head after the other, of
@@ -435,100 +465,7 @@ __device__ inline void diff_weights_and_grads(f32x16 &s1, f32x16 &s2, f32x16 &dp
 
 // dK and dV: a wavefront keeps 32 keys of one kv head and both gradients, and walks the queries of the group's heads.  What
 // lengths hide is the columns of keys behind the last, which are thrown away, and the rows of queries behind the last.
-template <int W>
-__global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
-    using T = float;
-    using Tile = DiffTile<T, W>;
-    constexpr int KS = W / 16, CB = W / 32;
-    __shared__ __align__(16) unsigned char smem[2][2][Tile::kBytes];
-    __shared__ __align__(16) float stats[2][4][kDiffTile];
-    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    DiffKeys p;
-    if (!p.find(a, wave, lane)) return;  // whole workgroup
-    DiffFrag<T> k[KS], v[KS];
-    {
-        const bool live = p.key < p.len_k;
-        const int at = live ? p.key : 0;
-        const T *krow = (const T *)a.k.ptr + p.b * a.k.sb + p.kv * a.k.sh + at * a.k.sn, *vrow = (const T *)a.v.ptr + p.b * a.v.sb + p.kv * a.v.sh + at * a.v.sn;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            k[ks] = diff_global_frag<T>(krow, ks, g, live);
-            v[ks] = diff_global_frag<T>(vrow, ks, g, live);
-        }
-    }
-    f32x16 dk[CB], dv[CB];
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-        diff_zero(dk[cb]);
-        diff_zero(dv[cb]);
-    }
-    DiffFetch<T, W, 256> qf, gf;
-    float stat = 0.f;
-    auto fetch = [&](int at) {
-        const int h = p.kv * a.group + at / p.n_tiles, row0 = (p.tile_begin + at % p.n_tiles) * kDiffTile;
-        qf.start(a.q.ptr, p.b * a.q.sb + h * a.q.sh, a.q.sn, tid);
-        gf.start(a.d_o.ptr, p.b * a.d_o.sb + h * a.d_o.sh, a.d_o.sn, tid);
-        qf.fetch(row0, p.len_q, tid);
-        gf.fetch(row0, p.len_q, tid);
-        if (tid < 128) stat = a.stats[(tid >> 5) * diff_rows(a) + ((long long)p.b * a.heads + h) * a.n_q + min(row0 + (tid & 31), a.n_q - 1)];
-    };
-    auto store = [&](int to) {
-        qf.store(smem[to][0], tid);
-        gf.store(smem[to][1], tid);
-        if (tid < 128) stats[to][tid >> 5][tid & 31] = stat;
-    };
-    if (p.from < p.to) {
-        fetch(p.from);
-        store(0);
-    }
-    lds_barrier();
-    float lam = 0.f;
-    int head = -1;
-    for (int at = p.from, buffer = 0; at < p.to; ++at, buffer ^= 1) {
-        if (at / p.n_tiles != head) {  // (uniform)
-            head = at / p.n_tiles;
-            lam = diff_lambda<W>(a, p.kv * a.group + head, lane).value;
-        }
-        const bool more = at + 1 < p.to;
-        if (more) fetch(at + 1);
-        const int tile = p.tile_begin + at % p.n_tiles;
-        if ((tile + 1) * kDiffTile > p.first_query) {  // (uniform in the wavefront)
-            const unsigned char *qt = smem[buffer][0], *gt = smem[buffer][1];
-            f32x16 s1, s2, dp;
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-                s1[x] = stats[buffer][0][8 * (x / 4) + 4 * g + x % 4];
-                s2[x] = stats[buffer][1][8 * (x / 4) + 4 * g + x % 4];
-                dp[x] = stats[buffer][2][8 * (x / 4) + 4 * g + x % 4];
-            }
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const DiffFrag<T> q = Tile::row_frag(qt, li, ks, g);
-                if (ks < KS / 2) s1 = diff_mma(q, k[ks], s1);
-                else s2 = diff_mma(q, k[ks], s2);
-            }
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) dp = diff_mma(Tile::row_frag(gt, li, ks, g), v[ks], dp);
-            if (p.masked(a, tile)) p.hide(a, s1, s2, tile, g);
-#pragma unroll
-            for (int x = 0; x < 16; ++x) diff_weights_and_grads(s1, s2, dp, x, stats[buffer][3][8 * (x / 4) + 4 * g + x % 4], a.c, lam);
-#pragma unroll
-            for (int kk = 0; kk < 2; ++kk) {
-                const DiffFrag<T> w = diff_block_frag<T>(dp, kk), ds1 = diff_block_frag<T>(s1, kk), ds2 = diff_block_frag<T>(s2, kk);
-#pragma unroll
-                for (int cb = 0; cb < CB; ++cb) {
-                    dv[cb] = diff_mma(Tile::col_frag(gt, kk, cb, lane), w, dv[cb]);
-                    dk[cb] = diff_mma(Tile::col_frag(qt, kk, cb, lane), cb < CB / 2 ? ds1 : ds2, dk[cb]);
-                }
-            }
-        }
-        if (more) store(buffer ^ 1);
-        lds_barrier();
-    }
-    diff_finish_dkv<T, W>(a, dk, dv, p, g);
-}
-
-// The same for bf16 tensors.  K operands stay in registers, V in LDS (with both gradients, 4 W / 32 accumulators of 16 registers, there
+// K operands stay in registers, V in LDS (with both gradients, 4 W / 32 accumulators of 16 registers, there
 // is no room for it at two wavefronts a SIMD); tiles of Q and dO and the queries' statistics come straight into two LDS stages, the
 // next tile's under this one's arithmetic.  Score products start from the stored logarithms and dP from -D1, read from LDS into the
 // accumulators.  LDS gives 40 + 8 KB a tile and wavefront for 4 W / 16 matrix instructions.
@@ -578,7 +515,7 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dkv_bf16_kernel(DiffArgs a) 
         const bool live = p.key < p.len_k;
         const __bf16 *row = (const __bf16 *)a.k.ptr + p.b * a.k.sb + p.kv * a.k.sh + (live ? p.key : 0) * a.k.sn;
 #pragma unroll
-        for (int ks = 0; ks < 2 * KS; ++ks) k[ks] = as_u32x4(diff_global_frag<__bf16>(row, ks, g, live).x);
+        for (int ks = 0; ks < 2 * KS; ++ks) k[ks] = as_u32x4(diff_global_frag(row, ks, g, live));
 #pragma unroll
         for (int ks = 0; ks < 2 * KS; ++ks) asm volatile("" : "+v"(k[ks]));  // (waited for here, not inside the loop)
         issue(0);
@@ -664,9 +601,9 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dkv_bf16_kernel(DiffArgs a) 
         bf16x8 w[2], ds1[2], ds2[2];
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
-            w[kk] = diff_block_frag<__bf16>(dp, kk).x;
-            ds1[kk] = diff_block_frag<__bf16>(s1, kk).x;
-            ds2[kk] = diff_block_frag<__bf16>(s2, kk).x;
+            w[kk] = diff_block_frag(dp, kk);
+            ds1[kk] = diff_block_frag(s1, kk);
+            ds2[kk] = diff_block_frag(s2, kk);
         }
         u32x2 c0[2 * CB], c1[2 * CB];
         Lds::template read_cols<TILE, 0>(c0, cols);
@@ -699,6 +636,165 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dkv_bf16_kernel(DiffArgs a) 
         lds_barrier();
     }
     diff_finish_dkv<__bf16, W>(a, dk, dv, p, g);
+}
+
+// The same for fp32 tensors, on operands of three bf16 numbers: K and V both in registers, one wavefront a SIMD.
+template <int W>
+__global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
+    using Lds = DiffLds<W>;
+    constexpr int KS = W / 32, CB = W / 32, TILE = DiffTile<W>::kBytes, STATS = 6 * kDiffTile * 4, STAGE = 6 * TILE + 1024;  // Q planes, dO planes, statistics
+    static_assert(STATS <= 1024, "stages stay 1 KB aligned");
+    __shared__ __align__(1024) unsigned char smem[2 * STAGE];
+    const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    DiffKeys p;
+    if (!p.find(a, wave, lane)) return;  // whole workgroup
+    int head = p.kv * a.group, tile = p.tile_begin;
+    if (p.n_tiles) {
+        head += p.from / p.n_tiles;
+        tile += p.from % p.n_tiles;
+    }
+    DiffDma3<W, 4> qload, gload;
+    int next_tile = tile, next_head = head;
+    qload.start(a.planes[0], ((long long)p.b * a.heads + head) * a.n_q, wave, lane);
+    gload.start(a.planes[3], ((long long)p.b * a.heads + head) * a.n_q, wave, lane);
+    // Loads of the next tile into a stage, and on to the one after.
+    auto issue = [&](int stage) {
+        unsigned char *to = smem + stage * STAGE;
+        const int row0 = next_tile * kDiffTile;
+        qload.issue(to, row0, p.len_q, wave, lane);
+        gload.issue(to + 3 * TILE, row0, p.len_q, wave, lane);
+        if (wave < 3) {  // statistics 2 wave and 2 wave + 1
+            const char *from = diff_uniform(a.stats + 2 * wave * diff_rows(a) + ((long long)p.b * a.heads + next_head) * a.n_q + row0);
+            const long long other = diff_rows(a) * 4;
+            const unsigned at = 4 * min(lane & 31, p.len_q - 1 - row0);
+            __builtin_amdgcn_global_load_lds((diff_global_cvoid *)(from + (lane >> 5) * other + at), (diff_lds_void *)(to + 6 * TILE + wave * 256), 4, 0, 0);
+        }
+        if (++next_tile == p.tile_begin + p.n_tiles) {
+            next_tile = p.tile_begin;
+            ++next_head;
+            qload.one.base += 6ll * W * a.n_q;
+            gload.one.base += 6ll * W * a.n_q;
+        }
+    };
+    if (p.from < p.to) issue(0);
+    DiffPlanes k[2 * KS], v[2 * KS];
+    {
+        const bool live = p.key < p.len_k;
+        const long long at = (((long long)p.b * a.kv_heads + p.kv) * a.n_k + (live ? p.key : 0)) * 3 * W;
+#pragma unroll
+        for (int ks = 0; ks < 2 * KS; ++ks) {
+            k[ks] = diff_global_planes<W>(a.planes[1] + at, ks, g, live);
+            v[ks] = diff_global_planes<W>(a.planes[2] + at, ks, g, live);
+        }
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2 * KS; ++ks)  // (waited for here, not inside the loop)
+        asm volatile("" : "+v"(k[ks].x[0]), "+v"(k[ks].x[1]), "+v"(k[ks].x[2]), "+v"(v[ks].x[0]), "+v"(v[ks].x[1]), "+v"(v[ks].x[2]));
+    f32x16 dk[CB], dv[CB];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+        diff_zero(dk[cb]);
+        diff_zero(dv[cb]);
+    }
+    const unsigned rows0 = Lds::rows(lds_address(smem), lane), cols0 = Lds::cols(lds_address(smem), lane), stats0 = lds_address(smem) + 6 * TILE + 16 * g;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    lds_barrier();
+    for (int at = p.from, stage = 0; at < p.to; ++at, stage ^= 1) {
+        if (at + 1 < p.to) issue(stage ^ 1);
+        const unsigned rows = rows0 + stage * STAGE, cols = cols0 + stage * STAGE, stats = stats0 + stage * STAGE;
+        f32x16 s1, s2, dp;
+        diff_zero(s1);
+        diff_zero(s2);
+        diff_zero(dp);
+        {
+            u32x4 x[2][3];
+            diff_read_rows3<W, 0>(x[0], rows, 0);
+            diff_landed(x[0]);
+#pragma unroll
+            for (int i = 0; i < 4 * KS; ++i) {  // Q operands, then dO operands
+                if (i + 1 < 2 * KS) diff_read_rows3<W, 0>(x[(i + 1) & 1], rows, i + 1);
+                else if (i + 1 < 4 * KS) diff_read_rows3<W, 3 * TILE>(x[(i + 1) & 1], rows, i + 1 - 2 * KS);
+                __builtin_amdgcn_sched_barrier(0);
+                bf16x8 q[3];
+                diff_rows3(x[i & 1], q);
+                if (i < KS) s1 = diff_mma6(q, k[i < KS ? i : 0].x, s1);
+                else if (i < 2 * KS) s2 = diff_mma6(q, k[i < 2 * KS ? i : 0].x, s2);
+                else dp = diff_mma6(q, v[i < 2 * KS ? 0 : i - 2 * KS].x, dp);
+                if (i + 1 < 4 * KS) diff_landed(x[(i + 1) & 1]);
+            }
+        }
+        if (p.masked(a, tile)) p.hide(a, s1, s2, tile, g);
+        // four rows' statistics at a time, the next four's on their way
+        {
+            u32x4 st[2][6];
+            auto read = [&](u32x4 (&to)[6], auto q4) {
+                constexpr int at0 = 32 * decltype(q4)::value, ROW = 4 * kDiffTile;
+                to[0] = lds_read_b128_at<at0>(stats);
+                to[1] = lds_read_b128_at<at0 + ROW>(stats);
+                to[2] = lds_read_b128_at<at0 + 2 * ROW>(stats);
+                to[3] = lds_read_b128_at<at0 + 3 * ROW>(stats);
+                to[4] = lds_read_b128_at<at0 + 4 * ROW>(stats);
+                to[5] = lds_read_b128_at<at0 + 5 * ROW>(stats);
+            };
+            auto landed = [](u32x4 (&x)[6]) {
+                asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]));
+            };
+            auto work = [&](const u32x4 (&x)[6], int q4) {
+                f32x4 y[6];
+#pragma unroll
+                for (int i = 0; i < 6; ++i) y[i] = __builtin_bit_cast(f32x4, x[i]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = 4 * q4 + e;
+                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s1[r], a.c, y[0][e])), e2 = __builtin_amdgcn_exp2f(fmaf(s2[r], a.c, y[1][e]));
+                    s1[r] = e1 * fmaf(dp[r], y[2][e], y[3][e]);
+                    s2[r] = e2 * fmaf(dp[r], y[4][e], y[5][e]);
+                    dp[r] = fmaf(e2, y[4][e], e1 * y[2][e]);
+                }
+            };
+            read(st[0], std::integral_constant<int, 0>());
+            landed(st[0]);
+            read(st[1], std::integral_constant<int, 1>());
+            __builtin_amdgcn_sched_barrier(0);
+            work(st[0], 0);
+            landed(st[1]);
+            read(st[0], std::integral_constant<int, 2>());
+            __builtin_amdgcn_sched_barrier(0);
+            work(st[1], 1);
+            landed(st[0]);
+            read(st[1], std::integral_constant<int, 3>());
+            __builtin_amdgcn_sched_barrier(0);
+            work(st[0], 2);
+            landed(st[1]);
+            work(st[1], 3);
+        }
+        // columns of dO for dV, then of Q for dK, 16 rows at a time
+        u32x2 c[2][6];
+        diff_read_cols3<W, 3 * TILE, 0>(c[0], cols, 0);
+        diff_landed(c[0]);
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            const DiffPlanes w = diff_block_planes(dp, kk), ds1 = diff_block_planes(s1, kk), ds2 = diff_block_planes(s2, kk);
+#pragma unroll
+            for (int i = 0; i < 2 * CB; ++i) {
+                const int cb = i % CB, j = kk * 2 * CB + i + 1;  // j: the next operand
+                if (j < CB) diff_read_cols3<W, 3 * TILE, 0>(c[j & 1], cols, j);
+                else if (j < 2 * CB) diff_read_cols3<W, 0, 0>(c[j & 1], cols, j - CB);
+                else if (j < 3 * CB) diff_read_cols3<W, 3 * TILE, 1>(c[j & 1], cols, j - 2 * CB);
+                else if (j < 4 * CB) diff_read_cols3<W, 0, 1>(c[j & 1], cols, j - 3 * CB);
+                __builtin_amdgcn_sched_barrier(0);
+                bf16x8 x[3];
+                diff_cols3(c[(j + 1) & 1], x);
+                if (i < CB) dv[cb] = diff_mma6(x, w.x, dv[cb]);
+                else dk[cb] = diff_mma6(x, cb < CB / 2 ? ds1.x : ds2.x, dk[cb]);
+                if (j < 4 * CB) diff_landed(c[j & 1]);
+            }
+        }
+        if (++tile == p.tile_begin + p.n_tiles) tile = p.tile_begin;  // on to the group's next head
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the next tile, for every wavefront, and every wavefront done with this one
+        lds_barrier();
+    }
+    diff_finish_dkv<float, W>(a, dk, dv, p, g);
 }
 
 // Parts of rows of `channels` fp32 numbers added in their order: row (x, h, n) of B x heads x n rows to tensor `out`, and its channels
@@ -767,7 +863,7 @@ static int diff_bwd_parts(long long items, long long tiles) {
 }
 struct DiffBwdPlan {
     int q_blocks, k_blocks, q_parts, k_parts;
-    size_t stats, lam, dq, dkv;  // bytes of the workspace's pieces, in this order
+    size_t stats, lam, dq, dkv, planes;  // bytes of the workspace's pieces, in this order
 };
 static DiffBwdPlan diff_bwd_plan(const jv_diff_attn_desc *d) {
     DiffBwdPlan p;
@@ -777,7 +873,8 @@ static DiffBwdPlan diff_bwd_plan(const jv_diff_attn_desc *d) {
     p.q_parts = diff_bwd_parts((long long)d->batch * d->heads * p.q_blocks, (d->n_k + kDiffTile - 1) / kDiffTile);
     p.k_parts = diff_bwd_parts((long long)d->batch * d->kv_heads * p.k_blocks, (d->n_q + kDiffTile - 1) / kDiffTile * group);
     auto whole = [](long long bytes) { return ((size_t)bytes + 255) & ~(size_t)255; };
-    p.stats = whole(rows * 16);
+    p.stats = whole(rows * (d->dtype == JV_BF16 ? 16 : 24));
+    p.planes = diff_planes_bytes(d, true);
     p.lam = whole((long long)d->batch * d->heads * p.q_blocks * p.q_parts * 4);
     p.dq = p.q_parts > 1 ? whole(rows * p.q_parts * d->head_dim * 4) : 0;
     p.dkv = p.k_parts > 1 ? whole(keys * p.k_parts * d->head_dim * 8) : 0;
@@ -785,13 +882,14 @@ static DiffBwdPlan diff_bwd_plan(const jv_diff_attn_desc *d) {
 }
 
 template <typename T, int W>
-static jv_status diff_backward(DiffArgs a, const DiffBwdPlan &plan, hipStream_t stream) {
+static jv_status diff_backward(DiffArgs a, const DiffBwdPlan &plan, void *planes, hipStream_t stream) {
     const long long rows = diff_rows(a), keys = (long long)a.B * a.kv_heads * a.n_k;
     constexpr int LANES = W * (int)sizeof(T) / 16;
     constexpr bool BF16 = sizeof(T) == 2;
     hipLaunchKernelGGL((diff_attn_rows_kernel<T, W>), dim3((unsigned)((rows * LANES + 255) / 256)), dim3(256), 0, stream, a);
     jv_status st = launch_status("diff_attn_rows_kernel");
     if (st != JV_OK) return st;
+    if (!BF16 && (st = diff_split(a, W, planes, true, stream)) != JV_OK) return st;
     a.blocks = plan.k_blocks;
     a.parts = plan.k_parts;
     a.items = (long long)a.B * a.kv_heads * a.blocks * a.parts;
@@ -828,7 +926,7 @@ size_t jv_diff_attn_bwd_workspace_bytes(const jv_diff_attn_desc *desc) {
     jv::clear_error();
     if (jv::diff_check_desc(desc) != JV_OK) return 0;
     const jv::DiffBwdPlan plan = jv::diff_bwd_plan(desc);
-    return plan.stats + plan.lam + plan.dq + plan.dkv;
+    return plan.stats + plan.lam + plan.dq + plan.dkv + plan.planes;
 }
 
 jv_status jv_diff_attn_bwd(const jv_diff_attn_desc *desc, const void *q, const void *k, const void *v,
@@ -888,9 +986,10 @@ jv_status jv_diff_attn_bwd(const jv_diff_attn_desc *desc, const void *q, const v
     p.a.lam_part = (float *)(at += plan.stats);
     p.a.dq_part = (float *)(at += plan.lam);
     p.a.dkv_part = (float *)(at += plan.dq);
+    at += plan.dkv;
     return jv::diff_with_kind(p.bf16, W, [&](auto kind) {
         using K = decltype(kind);
-        return jv::diff_backward<typename K::T, K::W>(p.a, plan, (hipStream_t)hip_stream);
+        return jv::diff_backward<typename K::T, K::W>(p.a, plan, at, (hipStream_t)hip_stream);
     });
 }
 
