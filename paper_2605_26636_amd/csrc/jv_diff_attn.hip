@@ -213,43 +213,60 @@ __device__ inline int diff_tiles(const DiffArgs &a, const DiffPlace &place, cons
 // Rows behind the last key are fetched as the last one, which is masked there.  Rows that see no key go along unmasked and are
 // dropped at the end.
 // ---------------------------------------------------------------------------------------
-// Weights of a tile packed to bf16, and the running softmax: see diff_softmax.
-__device__ inline float diff_exp_pack(unsigned (&pk)[8], const f32x16 &s, float c, float minus_m) {
+// Weights of a tile as bf16 numbers, TERMS = 1, or sums of two: rounded, and what rounding left.
+template <int TERMS>
+struct DiffWeights {
+    unsigned pk[TERMS][8];
+    __device__ void set(int v, float p0, float p1) {
+        pk[0][v] = pack_bf16x2(p0, p1);
+        if (TERMS == 2) pk[TERMS - 1][v] = pack_bf16x2(p0 - bf16_lo(pk[0][v]), p1 - bf16_hi(pk[0][v]));
+    }
+    __device__ bf16x8 frag(int term, int kk) const {
+        return as_bf16x8(u32x4{pk[term][4 * kk], pk[term][4 * kk + 1], pk[term][4 * kk + 2], pk[term][4 * kk + 3]});
+    }
+};
+// Weights of a tile and the running softmax: see diff_softmax.
+template <int TERMS>
+__device__ inline float diff_exp_pack(DiffWeights<TERMS> &w, const f32x16 &s, float c, float minus_m) {
     float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
     for (int v = 0; v < 8; ++v) {
         const float p0 = __builtin_amdgcn_exp2f(fmaf(s[2 * v], c, minus_m)), p1 = __builtin_amdgcn_exp2f(fmaf(s[2 * v + 1], c, minus_m));
-        pk[v] = pack_bf16x2(p0, p1);
+        w.set(v, p0, p1);
         sum0 += p0;
         sum1 += p1;
     }
     return sum0 + sum1;
 }
-template <int W>
-__device__ inline void diff_softmax_pack(DiffMap<W> &w, unsigned (&pk)[8], const f32x16 &s, float c) {
-    float sum = diff_exp_pack(pk, s, c, w.minus_m);
+template <int W, int TERMS>
+__device__ inline void diff_softmax_pack(DiffMap<W> &w, DiffWeights<TERMS> &p, const f32x16 &s, float c) {
+    float sum = diff_exp_pack(p, s, c, w.minus_m);
     if (__builtin_amdgcn_ballot_w64(!(sum <= kDiffLazySum)) != 0) {
         const float ref = diff_raise<W>(w, s, c);
         sum = 0.f;
 #pragma unroll
         for (int v = 0; v < 8; ++v) {
             const float p0 = diff_weight(s[2 * v], c, ref), p1 = diff_weight(s[2 * v + 1], c, ref);
-            pk[v] = pack_bf16x2(p0, p1);
+            p.set(v, p0, p1);
             sum += p0 + p1;
         }
     }
     w.l += sum;
 }
 
-template <typename TO, int W, int WAVES, bool SPLIT>
+// BOTH (up to 16 rows, one wavefront): lanes 0 .. 15 hold the rows for the first map and lanes 16 .. 31 for the second, each with zeros for the other map's
+// channels, so that a tile takes one block of scores, one softmax and half the products with V.  There is time for weights of
+// two terms then.
+template <typename TO, int W, int WAVES, bool SPLIT, bool BOTH = false>
 __global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffArgs a) {
+    static_assert(!BOTH || WAVES == 1, "a wavefront holds all rows twice");
     using Lds = DiffLds<W>;
     constexpr int KS = W / 32, CB = W / 32, TILE = kDiffTile * 2 * W, STAGE = 2 * TILE, RING = 3;  // a stage: K rows, then V rows
     __shared__ __align__(1024) unsigned char smem[RING * STAGE];
     __shared__ int wave_most[WAVES];
     const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     DiffPlace place;
-    if (!place.find<WAVES, SPLIT>(a, wave, li)) return;  // whole workgroup
+    if (!place.find<WAVES, SPLIT>(a, wave, BOTH ? li & 15 : li)) return;  // whole workgroup
     const DiffLengths len(a, place.b);
     int limit, least, tile, tile_end;
     const int sees = diff_tiles<WAVES, SPLIT>(a, place, len, wave_most, wave, lane, &limit, &least, &tile, &tile_end);
@@ -265,7 +282,7 @@ __global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffA
     {
         const __bf16 *row = (const __bf16 *)a.q.ptr + place.b * a.q.sb + place.head * a.q.sh + place.qi * a.q.sn;
 #pragma unroll
-        for (int ks = 0; ks < 2 * KS; ++ks) q[ks] = diff_global_frag(row, ks, g, sees > 0);
+        for (int ks = 0; ks < 2 * KS; ++ks) q[ks] = diff_global_frag(row, ks, g, sees > 0 && (!BOTH || (ks < KS) == (li < 16)));
     }
     if (tile < tile_end) issue(tile, 0);
     if (tile + 1 < tile_end) issue(tile + 1, 1);
@@ -296,7 +313,10 @@ __global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffA
         for (int ks = 0; ks < KS; ++ks) s1 = mfma32(as_bf16x8(k1[ks]), q[ks], s1);
         diff_landed(k2);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s2 = mfma32(as_bf16x8(k2[ks]), q[KS + ks], s2);
+        for (int ks = 0; ks < KS; ++ks) {
+            if (BOTH) s1 = mfma32(as_bf16x8(k2[ks]), q[KS + ks], s1);
+            else s2 = mfma32(as_bf16x8(k2[ks]), q[KS + ks], s2);
+        }
         __builtin_amdgcn_sched_barrier(0);
         // the next tile has landed for every wavefront, and every wavefront has left the tile before, whose stage takes the one after
         if (tile + 1 < tile_end) {
@@ -305,20 +325,22 @@ __global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffA
             if (tile + 2 < tile_end) issue(tile + 2, after);
         }
         if ((tile + 1) * kDiffTile > least) diff_hide_keys(s1, s2, tile * kDiffTile, limit, g);
-        unsigned p1[8], p2[8];
-        diff_softmax_pack<W>(w1, p1, s1, a.c);
+        constexpr int TERMS = BOTH ? 2 : 1;
+        DiffWeights<TERMS> p1, p2;
+        diff_softmax_pack(w1, p1, s1, a.c);
         u32x2 v0[2 * CB];
         Lds::template read_cols<TILE, 0>(v0, vat);
         __builtin_amdgcn_sched_barrier(0);
-        diff_softmax_pack<W>(w2, p2, s2, a.c);
+        if (!BOTH) diff_softmax_pack(w2, p2, s2, a.c);
         auto products = [&](const u32x2 (&v)[2 * CB], int kk) {
-            const bf16x8 b1 = as_bf16x8(u32x4{p1[4 * kk], p1[4 * kk + 1], p1[4 * kk + 2], p1[4 * kk + 3]});
-            const bf16x8 b2 = as_bf16x8(u32x4{p2[4 * kk], p2[4 * kk + 1], p2[4 * kk + 2], p2[4 * kk + 3]});
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb) {
                 const bf16x8 x = diff_join2(v[2 * cb], v[2 * cb + 1]);
-                w1.acc[cb] = mfma32(x, b1, w1.acc[cb]);
-                w2.acc[cb] = mfma32(x, b2, w2.acc[cb]);
+#pragma unroll
+                for (int t = TERMS - 1; t >= 0; --t) {
+                    w1.acc[cb] = mfma32(x, p1.frag(t, kk), w1.acc[cb]);
+                    if (!BOTH) w2.acc[cb] = mfma32(x, p2.frag(t, kk), w2.acc[cb]);
+                }
             }
         };
         diff_landed(v0);
@@ -336,10 +358,19 @@ __global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffA
     }
     int l = lane;
     asm("" : "+v"(l));  // (where the rows lie is worked out again: kept across the loop it would cost registers that are missed there)
-    place.find<WAVES, SPLIT>(a, wave, l & 31);
+    place.find<WAVES, SPLIT>(a, wave, BOTH ? l & 15 : l & 31);
     if ((place.row_live ? len.limit(a, place.qi) : 0) == 0) {
         w1.clear();
         w2.clear();
+    }
+    if (BOTH) {  // the second map comes to the lanes of the first
+        w2.m = __shfl_xor(w1.m, 16);
+        w2.l = __shfl_xor(w1.l, 16);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) w2.acc[cb][v] = __shfl_xor(w1.acc[cb][v], 16);
+        place.row_live = place.row_live && (l & 16) == 0;
     }
     diff_finish<__bf16, TO, W, SPLIT>(a, place, w1, w2, l);
 }
@@ -491,18 +522,79 @@ jv_status diff_split(DiffArgs &a, int W, void *memory, bool with_d_o, hipStream_
     return launch_status("diff_attn_split_kernel");
 }
 
-// The parts of a row joined by SHARE wavefronts, which take every SHARE-th part each, eight parts' loads at a time (parts that saw no key are
-// read, in bounds, and not used), and are added in their order.  Four wavefronts a row where there are many parts: one query token
-// against 16 384 keys x 8 sequences x 16 heads in 24 parts 6 us, in 39 with one wavefront and one part after the other 21;
-// 576 tokens x 24 heads in 4 parts 25 us with four wavefronts a row, 11 with one.
-template <typename T, typename TO, int W, int SHARE>
+// The parts of a row joined, in their order; a part that saw no key is read, in bounds, and not used.
+// Up to eight parts: a wavefront a row, everything it needs of all parts asked for at once (576 tokens x 24 heads in two parts 6 us; 11 with the parts'
+// references first, exchanged between lanes).
+constexpr int kDiffFewParts = 8;
+// Where row `at` of all (batch, kv head, row)s lies.
+struct DiffRowPlace {
+    int b, head, qi;
+    long long row;
+    __device__ DiffRowPlace(const DiffArgs &a, long long at) {
+        const int n_rows = a.group * a.n_q, bkv = (int)(at / n_rows), r = (int)(at % n_rows), hg = r / a.n_q;
+        b = bkv / a.kv_heads;
+        qi = r - hg * a.n_q;
+        head = bkv % a.kv_heads * a.group + hg;
+        row = ((long long)b * a.heads + head) * a.n_q + qi;
+    }
+};
+template <typename T, typename TO, int W>
+__global__ void __launch_bounds__(256) diff_attn_join_few_kernel(DiffArgs a) {
+    constexpr int PER = W / 64;  // channels a lane
+    const int lane = threadIdx.x & 63;
+    const long long all = diff_rows(a), at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (at >= all) return;
+    const DiffRowPlace place(a, at);
+    f32x4 ml[kDiffFewParts];
+    float x1[kDiffFewParts][PER], x2[kDiffFewParts][PER];
+#pragma unroll
+    for (int s = 0; s < kDiffFewParts; ++s) {
+        const float *part = a.part + ((long long)min(s, a.splits - 1) * all + at) * (2 * W + 4);
+        ml[s] = *(const f32x4 *)part;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            x1[s][e] = part[4 + lane * PER + e];
+            x2[s][e] = part[4 + W + lane * PER + e];
+        }
+    }
+    const float lam = diff_lambda<W>(a, place.head, lane).value;
+    float m1 = -INFINITY, m2 = -INFINITY, l1 = 0.f, l2 = 0.f, y1[PER] = {}, y2[PER] = {};
+#pragma unroll
+    for (int s = 0; s < kDiffFewParts; ++s) {
+        m1 = fmaxf(m1, ml[s][0]);
+        m2 = fmaxf(m2, ml[s][2]);
+    }
+#pragma unroll
+    for (int s = 0; s < kDiffFewParts; ++s) {
+        if (s >= a.splits || ml[s][0] == -INFINITY) continue;  // (uniform; both maps see the same keys)
+        const float f1 = __builtin_amdgcn_exp2f(ml[s][0] - m1), f2 = __builtin_amdgcn_exp2f(ml[s][2] - m2);
+        l1 = fmaf(ml[s][1], f1, l1);
+        l2 = fmaf(ml[s][3], f2, l2);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            y1[e] = fmaf(x1[s][e], f1, y1[e]);
+            y2[e] = fmaf(x2[s][e], f2, y2[e]);
+        }
+    }
+    if (a.ml && lane == 0) diff_save(a, place.row, m1, l1, m2, l2);
+    const float inv1 = l1 > 0.f ? 1.f / l1 : l1, inv2 = l2 > 0.f ? 1.f / l2 : l2;
+    TO *o = (TO *)const_cast<void *>(a.o.ptr) + place.b * a.o.sb + place.head * a.o.sh + place.qi * a.o.sn + lane * PER;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        const float y = y2[e] * inv2;
+        o[e] = (TO)fmaf(-lam, y, y1[e] * inv1);
+        if (a.o2) ((T *)a.o2)[place.row * W + lane * PER + e] = (T)y;
+    }
+}
+
+// More parts, up to 64: a workgroup a row, whose four wavefronts take every fourth part each, eight parts' loads at a time (one query token
+// against 16 384 keys x 8 sequences x 16 heads in 24 parts 6 us; in 39 by one wavefront, one part after the other, 21).
+template <typename T, typename TO, int W>
 __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, turn = wave % SHARE, n_rows = a.group * a.n_q;
-    const long long all = (long long)a.B * a.kv_heads * n_rows, at = (long long)blockIdx.x * (4 / SHARE) + wave / SHARE;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const long long all = diff_rows(a), at = blockIdx.x;
     __shared__ float sums[4][2 * W];
-    if (SHARE == 1 && at >= all) return;
-    const int bkv = (int)(at / n_rows), r = (int)(at % n_rows), b = bkv / a.kv_heads, kv = bkv % a.kv_heads;
-    const int hg = r / a.n_q, qi = r - hg * a.n_q, head = kv * a.group + hg;
+    const DiffRowPlace place(a, at);
     f32x4 ml = {-INFINITY, 0.f, -INFINITY, 0.f};
     if (lane < a.splits) ml = *(const f32x4 *)(a.part + ((long long)lane * all + at) * (2 * W + 4));
     float m1 = ml[0], m2 = ml[2];
@@ -513,12 +605,12 @@ __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
     }
     const float f1 = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m1), f2 = ml[2] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[2] - m2);
     const float l1 = wave_sum(ml[1] * f1), l2 = wave_sum(ml[3] * f2);
-    const unsigned long long seen = __builtin_amdgcn_ballot_w64(ml[0] != -INFINITY || ml[2] != -INFINITY);
+    const unsigned long long seen = __builtin_amdgcn_ballot_w64(ml[0] != -INFINITY);
     constexpr int PER = W / 32;  // channels a lane: lanes 0 .. 31 those of the first map, 32 .. 63 of the second
     float x[PER] = {};
     const float *part = a.part + at * (2 * W + 4) + 4 + lane * PER;
 #pragma unroll 8
-    for (int s = turn; s < a.splits; s += SHARE) {
+    for (int s = wave; s < a.splits; s += 4) {
         float y[PER];
 #pragma unroll
         for (int e = 0; e < PER; ++e) y[e] = part[s * all * (2 * W + 4) + e];
@@ -528,24 +620,16 @@ __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
     }
 #pragma unroll
     for (int e = 0; e < PER; ++e) sums[wave][lane * PER + e] = x[e];
-    const float lam = diff_lambda<W>(a, head, lane).value;
-    if (SHARE > 1) __syncthreads();
-    else __builtin_amdgcn_wave_barrier();  // (a wavefront's own LDS operations keep their order)
-    const long long row = ((long long)b * a.heads + head) * a.n_q + qi;
-    if (a.ml && turn == 0 && lane == 0) diff_save(a, row, m1, l1, m2, l2);
+    const float lam = diff_lambda<W>(a, place.head, lane).value;
+    __syncthreads();
+    const int ch = threadIdx.x;
+    if (a.ml && ch == 0) diff_save(a, place.row, m1, l1, m2, l2);
+    if (ch >= W) return;
     const float inv1 = l1 > 0.f ? 1.f / l1 : l1, inv2 = l2 > 0.f ? 1.f / l2 : l2;
-    TO *o = (TO *)const_cast<void *>(a.o.ptr) + b * a.o.sb + head * a.o.sh + qi * a.o.sn;
-    for (int ch = turn * 64 + lane; ch < W; ch += 64 * SHARE) {
-        float y1 = 0.f, y2 = 0.f;
-#pragma unroll
-        for (int w = 0; w < SHARE; ++w) {
-            y1 += sums[wave - turn + w][ch];
-            y2 += sums[wave - turn + w][W + ch];
-        }
-        y2 *= inv2;
-        o[ch] = (TO)fmaf(-lam, y2, y1 * inv1);
-        if (a.o2) ((T *)a.o2)[row * W + ch] = (T)y2;
-    }
+    const float y1 = ((sums[0][ch] + sums[1][ch]) + (sums[2][ch] + sums[3][ch])) * inv1;
+    const float y2 = ((sums[0][W + ch] + sums[1][W + ch]) + (sums[2][W + ch] + sums[3][W + ch])) * inv2;
+    ((TO *)const_cast<void *>(a.o.ptr) + place.b * a.o.sb + place.head * a.o.sh + place.qi * a.o.sn)[ch] = (TO)fmaf(-lam, y2, y1);
+    if (a.o2) ((T *)a.o2)[place.row * W + ch] = (T)y2;
 }
 
 // ---------------------------------------------------------------------------------------
@@ -554,20 +638,20 @@ __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
 
 // How a forward pass is cut: wavefronts a workgroup (32 rows each) and parts of the keys.  Up to 64 rows (a few queries, all heads
 // of a group together) take one wavefront each; more take workgroups of four, which share the tiles.  Keys are cut where
-// the launch would leave units idle: into as many parts as the chip holds workgroups at a time (single wavefronts: three a unit
-// for their 48 KB of LDS; one query token against 16 384 keys x 8 sequences 53 us in 2 048 of them, 41 in 768), of four tiles at
-// least, at most 64 (a wavefront of the join holds one part a lane).
+// the launch would leave units idle: into as many parts as the chip holds workgroups at a time (single wavefronts: as their 24 to 96 KB of LDS let
+// on a unit; one query token against 16 384 keys x 8 sequences 53 us in 2 048 of them, 41 in 768), of four tiles at
+// least, one of fp32 tensors, whose tiles take 2 us (256 tokens x 6 heads in parts of four 15.8 us), at most 64 (a wavefront of the join holds one part a lane).
 struct DiffPlan {
     int waves, blocks, splits, tiles_per_split;
 };
-static DiffPlan diff_plan(int B, int kv_heads, long long n_rows, int n_k, bool bf16) {
+static DiffPlan diff_plan(int B, int kv_heads, long long n_rows, int n_k, int W, bool bf16) {
     DiffPlan p;
     p.waves = n_rows <= 64 ? 1 : 4;
     p.blocks = (int)((n_rows + 32 * p.waves - 1) / (32 * p.waves));
     const long long groups = (long long)B * kv_heads * p.blocks, tiles = (n_k + kDiffTile - 1) / kDiffTile;
-    const long long want = p.waves == 1 ? 768 : bf16 ? 512 : 256;
-    long long splits = groups * 2 > want ? 1 : want / groups;
-    splits = std::max(1ll, std::min({splits, tiles / 4, 64ll}));
+    const long long holds = p.waves == 1 ? (bf16 || W == 64 ? 768 : 256) : bf16 ? 512 : 256;
+    long long splits = groups * 2 > holds ? 1 : holds / groups;
+    splits = std::max(1ll, std::min({splits, bf16 ? tiles / 4 : tiles, 64ll}));
     p.tiles_per_split = (int)((tiles + splits - 1) / splits);
     p.splits = (int)((tiles + p.tiles_per_split - 1) / p.tiles_per_split);
     return p;
@@ -629,7 +713,7 @@ jv_status diff_check_desc(const jv_diff_attn_desc *d) {
 }
 
 static DiffPlan diff_plan_of(const jv_diff_attn_desc *d) {
-    return diff_plan(d->batch, d->kv_heads, (long long)d->heads / d->kv_heads * d->n_q, d->n_k, d->dtype == JV_BF16);
+    return diff_plan(d->batch, d->kv_heads, (long long)d->heads / d->kv_heads * d->n_q, d->n_k, d->head_dim, d->dtype == JV_BF16);
 }
 
 size_t diff_saved_bytes(const jv_diff_attn_desc *d) {
@@ -697,6 +781,12 @@ static jv_status diff_forward(DiffArgs a, const DiffPlan &plan, void *planes, hi
         constexpr int WAVES = decltype(waves)::value;
         constexpr bool SPLIT = decltype(split)::value;
         using Out = std::conditional_t<SPLIT, float, TO>;
+        if constexpr (sizeof(T) == 2 && WAVES == 1) {
+            if (a.group * (long long)a.n_q <= 16) {
+                hipLaunchKernelGGL((diff_attn_fwd_bf16_kernel<Out, W, 1, SPLIT, true>), grid, dim3(64), 0, stream, a);
+                return;
+            }
+        }
         if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((diff_attn_fwd_bf16_kernel<Out, W, WAVES, SPLIT>), grid, dim3(64 * WAVES), 0, stream, a);
         else hipLaunchKernelGGL((diff_attn_fwd_f32_kernel<W, WAVES, SPLIT>), grid, dim3(64 * WAVES), 0, stream, a);
     };
@@ -709,8 +799,8 @@ static jv_status diff_forward(DiffArgs a, const DiffPlan &plan, void *planes, hi
     else launch(std::integral_constant<int, 4>(), std::true_type());
     if ((st = launch_status("diff_attn_fwd_kernel")) != JV_OK) return st;
     const long long rows = diff_rows(a);
-    if (a.splits > 8) hipLaunchKernelGGL((diff_attn_join_kernel<T, TO, W, 4>), dim3((unsigned)rows), dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((diff_attn_join_kernel<T, TO, W, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a);
+    if (a.splits > kDiffFewParts) hipLaunchKernelGGL((diff_attn_join_kernel<T, TO, W>), dim3((unsigned)rows), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((diff_attn_join_few_kernel<T, TO, W>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a);
     return launch_status("diff_attn_join_kernel");
 }
 
