@@ -383,7 +383,8 @@ template <int W, int WAVES, bool SPLIT>
 __global__ void __launch_bounds__(64 * WAVES, W == 64 && WAVES > 1 ? 2 : 1) diff_attn_fwd_f32_kernel(DiffArgs a) {
     using Lds = DiffLds<W>;
     constexpr int KS = W / 32, CB = W / 32, TILE = DiffTile<W>::kBytes, STAGE = 6 * TILE;  // a stage: three planes of K rows, three of V rows
-    __shared__ __align__(1024) unsigned char smem[2 * STAGE];
+    constexpr int STAGES = WAVES == 1 ? 1 : 2;  // (single wavefronts: three on a unit in place of one, each under the others' loads)
+    __shared__ __align__(1024) unsigned char smem[STAGES * STAGE];
     __shared__ int wave_most[WAVES];
     const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, li = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     DiffPlace place;
@@ -414,8 +415,8 @@ __global__ void __launch_bounds__(64 * WAVES, W == 64 && WAVES > 1 ? 2 : 1) diff
     const unsigned rows0 = Lds::rows(lds_address(smem), lane), cols0 = Lds::cols(lds_address(smem), lane);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     lds_barrier();
-    for (int stage = 0; tile < tile_end; ++tile, stage ^= 1) {
-        if (tile + 1 < tile_end) issue(tile + 1, stage ^ 1);
+    for (int stage = 0; tile < tile_end; ++tile, stage ^= STAGES - 1) {
+        if (STAGES == 2 && tile + 1 < tile_end) issue(tile + 1, stage ^ 1);
         const unsigned rows = rows0 + stage * STAGE, cols = cols0 + stage * STAGE;
         f32x16 s1, s2, p;
         diff_zero(s1);
@@ -459,6 +460,7 @@ __global__ void __launch_bounds__(64 * WAVES, W == 64 && WAVES > 1 ? 2 : 1) diff
             w2.acc[cb] = diff_mma6(x, p2[kk].x, w2.acc[cb]);
             if (i + 1 < 2 * CB) diff_landed(v[(i + 1) & 1]);
         }
+        if (STAGES == 1 && tile + 1 < tile_end) issue(tile + 1, 0);  // (its own LDS reads have landed)
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the next tile, for every wavefront, and every wavefront done with this one
         lds_barrier();
     }
@@ -638,9 +640,10 @@ __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
 
 // How a forward pass is cut: wavefronts a workgroup (32 rows each) and parts of the keys.  Up to 64 rows (a few queries, all heads
 // of a group together) take one wavefront each; more take workgroups of four, which share the tiles.  Keys are cut where
-// the launch would leave units idle: into as many parts as the chip holds workgroups at a time (single wavefronts: as their 24 to 96 KB of LDS let
-// on a unit; one query token against 16 384 keys x 8 sequences 53 us in 2 048 of them, 41 in 768), of four tiles at
-// least, one of fp32 tensors, whose tiles take 2 us (256 tokens x 6 heads in parts of four 15.8 us), at most 64 (a wavefront of the join holds one part a lane).
+// the launch would leave units idle: into as many parts as the chip holds workgroups at a time (single wavefronts: three or six a unit, as their
+// LDS lets; one query token against 16 384 keys x 8 sequences 53 us in 2 048 of them, 41 in 768), at most 64 (a wavefront of
+// the join holds one part a lane).  Two and four tiles at least, us: one query against 2 x 1 374 keys x 16 heads 11.3 / 12.3, against 300 x 8 11.0 / 14.4, against
+// 4 x 4 096 x 16 19.6 / 18.7 (48 and 32 parts), 40 queries against 2 x 1 024 x 8 14.2 / 12.1, 577 tokens x 8 25.8 / 24.3.
 struct DiffPlan {
     int waves, blocks, splits, tiles_per_split;
 };
@@ -649,9 +652,12 @@ static DiffPlan diff_plan(int B, int kv_heads, long long n_rows, int n_k, int W,
     p.waves = n_rows <= 64 ? 1 : 4;
     p.blocks = (int)((n_rows + 32 * p.waves - 1) / (32 * p.waves));
     const long long groups = (long long)B * kv_heads * p.blocks, tiles = (n_k + kDiffTile - 1) / kDiffTile;
-    const long long holds = p.waves == 1 ? (bf16 || W == 64 ? 768 : 256) : bf16 ? 512 : 256;
+    const bool both = bf16 && n_rows <= 16;
+    const long long holds = p.waves == 1 ? (bf16 || W == 128 ? 768 : 1536) : bf16 ? 512 : 256;
+    // tiles of a part: four of bf16 tensors (of few rows two, up to 24 parts), one of fp32 ones, whose tiles take 2 us and more
+    const long long most = !bf16 ? tiles : both ? std::max(tiles / 4, std::min(tiles / 2, 24ll)) : tiles / 4;
     long long splits = groups * 2 > holds ? 1 : holds / groups;
-    splits = std::max(1ll, std::min({splits, bf16 ? tiles / 4 : tiles, 64ll}));
+    splits = std::max(1ll, std::min({splits, most, 64ll}));
     p.tiles_per_split = (int)((tiles + splits - 1) / splits);
     p.splits = (int)((tiles + p.tiles_per_split - 1) / p.tiles_per_split);
     return p;
