@@ -855,11 +855,12 @@ __global__ void __launch_bounds__(1024) diff_attn_dlambda_kernel(DiffArgs a) {
     }
 }
 
-// Parts of the tiles that the workgroups of a pass are cut into: as many as bring `items` workgroups (of which a chip holds 512) to
-// 1 024, of eight tiles at least, 16 at most.
-static int diff_bwd_parts(long long items, long long tiles) {
-    const long long parts = items >= 512 ? 1 : (1024 + items - 1) / items;
-    return (int)std::max(1ll, std::min({parts, tiles / 8, 16ll}));
+// Parts of the tiles that the workgroups of a pass are cut into where they do not fill the chip (512 of bf16 tensors at a time, 256 of fp32
+// ones): as many as fill it, twice that where a causal mask makes some much longer than others; of four tiles at least, of two of fp32
+// tensors, 16 at most.
+static int diff_bwd_parts(long long items, long long tiles, bool bf16, bool causal) {
+    const long long holds = (bf16 ? 512 : 256) * (causal ? 2 : 1);
+    return (int)std::max(1ll, std::min({holds / items, tiles / (bf16 ? 4 : 2), 16ll}));
 }
 struct DiffBwdPlan {
     int q_blocks, k_blocks, q_parts, k_parts;
@@ -870,8 +871,8 @@ static DiffBwdPlan diff_bwd_plan(const jv_diff_attn_desc *d) {
     p.q_blocks = (d->n_q + 127) / 128;
     p.k_blocks = (d->n_k + 127) / 128;
     const long long group = d->heads / d->kv_heads, rows = (long long)d->batch * d->heads * d->n_q, keys = (long long)d->batch * d->kv_heads * d->n_k;
-    p.q_parts = diff_bwd_parts((long long)d->batch * d->heads * p.q_blocks, (d->n_k + kDiffTile - 1) / kDiffTile);
-    p.k_parts = diff_bwd_parts((long long)d->batch * d->kv_heads * p.k_blocks, (d->n_q + kDiffTile - 1) / kDiffTile * group);
+    p.q_parts = diff_bwd_parts((long long)d->batch * d->heads * p.q_blocks, (d->n_k + kDiffTile - 1) / kDiffTile, d->dtype == JV_BF16, d->causal);
+    p.k_parts = diff_bwd_parts((long long)d->batch * d->kv_heads * p.k_blocks, (d->n_q + kDiffTile - 1) / kDiffTile * group, d->dtype == JV_BF16, d->causal);
     auto whole = [](long long bytes) { return ((size_t)bytes + 255) & ~(size_t)255; };
     p.stats = whole(rows * (d->dtype == JV_BF16 ? 16 : 24));
     p.planes = diff_planes_bytes(d, true);
