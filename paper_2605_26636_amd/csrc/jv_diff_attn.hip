@@ -525,8 +525,7 @@ jv_status diff_split(DiffArgs &a, int W, void *memory, bool with_d_o, hipStream_
 }
 
 // The parts of a row joined, in their order; a part that saw no key is read, in bounds, and not used.
-// Up to eight parts: a wavefront a row, everything it needs of all parts asked for at once (576 tokens x 24 heads in two parts 6 us; 11 with the parts'
-// references first, exchanged between lanes).
+// Up to PARTS (2, 4 or 8) parts: a wavefront a row, everything it needs of all parts asked for at once.
 constexpr int kDiffFewParts = 8;
 // Where row `at` of all (batch, kv head, row)s lies.
 struct DiffRowPlace {
@@ -540,17 +539,17 @@ struct DiffRowPlace {
         row = ((long long)b * a.heads + head) * a.n_q + qi;
     }
 };
-template <typename T, typename TO, int W>
+template <typename T, typename TO, int W, int PARTS>
 __global__ void __launch_bounds__(256) diff_attn_join_few_kernel(DiffArgs a) {
     constexpr int PER = W / 64;  // channels a lane
     const int lane = threadIdx.x & 63;
     const long long all = diff_rows(a), at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (at >= all) return;
     const DiffRowPlace place(a, at);
-    f32x4 ml[kDiffFewParts];
-    float x1[kDiffFewParts][PER], x2[kDiffFewParts][PER];
+    f32x4 ml[PARTS];
+    float x1[PARTS][PER], x2[PARTS][PER];
 #pragma unroll
-    for (int s = 0; s < kDiffFewParts; ++s) {
+    for (int s = 0; s < PARTS; ++s) {
         const float *part = a.part + ((long long)min(s, a.splits - 1) * all + at) * (2 * W + 4);
         ml[s] = *(const f32x4 *)part;
 #pragma unroll
@@ -562,12 +561,12 @@ __global__ void __launch_bounds__(256) diff_attn_join_few_kernel(DiffArgs a) {
     const float lam = diff_lambda<W>(a, place.head, lane).value;
     float m1 = -INFINITY, m2 = -INFINITY, l1 = 0.f, l2 = 0.f, y1[PER] = {}, y2[PER] = {};
 #pragma unroll
-    for (int s = 0; s < kDiffFewParts; ++s) {
+    for (int s = 0; s < PARTS; ++s) {
         m1 = fmaxf(m1, ml[s][0]);
         m2 = fmaxf(m2, ml[s][2]);
     }
 #pragma unroll
-    for (int s = 0; s < kDiffFewParts; ++s) {
+    for (int s = 0; s < PARTS; ++s) {
         if (s >= a.splits || ml[s][0] == -INFINITY) continue;  // (uniform; both maps see the same keys)
         const float f1 = __builtin_amdgcn_exp2f(ml[s][0] - m1), f2 = __builtin_amdgcn_exp2f(ml[s][2] - m2);
         l1 = fmaf(ml[s][1], f1, l1);
@@ -805,8 +804,11 @@ static jv_status diff_forward(DiffArgs a, const DiffPlan &plan, void *planes, hi
     else launch(std::integral_constant<int, 4>(), std::true_type());
     if ((st = launch_status("diff_attn_fwd_kernel")) != JV_OK) return st;
     const long long rows = diff_rows(a);
-    if (a.splits > kDiffFewParts) hipLaunchKernelGGL((diff_attn_join_kernel<T, TO, W>), dim3((unsigned)rows), dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((diff_attn_join_few_kernel<T, TO, W>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a);
+    const dim3 few((unsigned)((rows + 3) / 4));
+    if (a.splits <= 2) hipLaunchKernelGGL((diff_attn_join_few_kernel<T, TO, W, 2>), few, dim3(256), 0, stream, a);
+    else if (a.splits <= 4) hipLaunchKernelGGL((diff_attn_join_few_kernel<T, TO, W, 4>), few, dim3(256), 0, stream, a);
+    else if (a.splits <= kDiffFewParts) hipLaunchKernelGGL((diff_attn_join_few_kernel<T, TO, W, kDiffFewParts>), few, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((diff_attn_join_kernel<T, TO, W>), dim3((unsigned)rows), dim3(256), 0, stream, a);
     return launch_status("diff_attn_join_kernel");
 }
 
