@@ -389,6 +389,8 @@ def jv_diff_attn_bwd_workspace_bytes(desc):
 
 
 def _sized(t):
+    if t is not None and not t.is_contiguous():
+        raise ValueError("saved and workspace must be contiguous")
     return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
 
 

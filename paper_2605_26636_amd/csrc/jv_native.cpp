@@ -202,13 +202,13 @@ bool bool_arg(PyObject *obj, bool *out) {
     *out = x > 0;
     return x >= 0;
 }
-// Memory of a number of bytes, or None.
+// Memory of a number of bytes (a tensor without gaps), or None.
 bool memory_arg(PyObject *obj, void **ptr, size_t *bytes) {
     bool absent;
     const at::Tensor *t = device_tensor(obj, nullptr, &absent);
     *ptr = t ? t->data_ptr() : nullptr;
     *bytes = t ? t->nbytes() : 0;
-    return t || absent;
+    return absent || (t && t->is_contiguous());
 }
 bool strided_arg(const at::Tensor *t, jv_strides *out, const at::Tensor *like = nullptr) {
     if (!t || t->dim() != 4 || t->stride(3) != 1 || (like && t->sizes() != like->sizes())) return false;
