@@ -12,6 +12,7 @@
 
 #include "jv_common.h"
 #include "jv_mfma.h"
+#include "jv_plan.h"
 
 namespace jv {
 
@@ -72,8 +73,6 @@ struct DiffItem {
     }
 };
 inline unsigned diff_grid(long long items) { return (unsigned)(8 * ((items + 7) / 8)); }
-
-constexpr int kDiffTile = 32;  // tokens of a tile
 
 // Tokens [0, limit) of a sequence that query qi sees, by the lengths of the sequence.
 struct DiffLengths {

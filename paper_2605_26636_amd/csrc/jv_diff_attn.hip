@@ -637,30 +637,6 @@ __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
 // Host side
 // ---------------------------------------------------------------------------------------
 
-// How a forward pass is cut: wavefronts a workgroup (32 rows each) and parts of the keys.  Up to 64 rows (a few queries, all heads
-// of a group together) take one wavefront each; more take workgroups of four, which share the tiles.  Keys are cut where
-// the launch would leave units idle: into as many parts as the chip holds workgroups at a time (single wavefronts: three or six a unit, as their
-// LDS lets; one query token against 16 384 keys x 8 sequences 53 us in 2 048 of them, 41 in 768), at most 64 (a wavefront of
-// the join holds one part a lane).  Two and four tiles at least, us: one query against 2 x 1 374 keys x 16 heads 11.3 / 12.3, against 300 x 8 11.0 / 14.4, against
-// 4 x 4 096 x 16 19.6 / 18.7 (48 and 32 parts), 40 queries against 2 x 1 024 x 8 14.2 / 12.1, 577 tokens x 8 25.8 / 24.3.
-struct DiffPlan {
-    int waves, blocks, splits, tiles_per_split;
-};
-static DiffPlan diff_plan(int B, int kv_heads, long long n_rows, int n_k, int W, bool bf16) {
-    DiffPlan p;
-    p.waves = n_rows <= 64 ? 1 : 4;
-    p.blocks = (int)((n_rows + 32 * p.waves - 1) / (32 * p.waves));
-    const long long groups = (long long)B * kv_heads * p.blocks, tiles = (n_k + kDiffTile - 1) / kDiffTile;
-    const bool both = bf16 && n_rows <= 16;
-    const long long holds = p.waves == 1 ? (bf16 || W == 128 ? 768 : 1536) : bf16 ? 512 : 256;
-    // tiles of a part: four of bf16 tensors (of few rows two, up to 24 parts), one of fp32 ones, whose tiles take 2 us and more
-    const long long most = !bf16 ? tiles : both ? std::max(tiles / 4, std::min(tiles / 2, 24ll)) : tiles / 4;
-    long long splits = groups * 2 > holds ? 1 : holds / groups;
-    splits = std::max(1ll, std::min({splits, most, 64ll}));
-    p.tiles_per_split = (int)((tiles + splits - 1) / splits);
-    p.splits = (int)((tiles + p.tiles_per_split - 1) / p.tiles_per_split);
-    return p;
-}
 static size_t diff_part_bytes(const DiffPlan &p, long long rows, int W) {
     return p.splits > 1 ? (size_t)p.splits * rows * (2 * W + 4) * 4 : 0;
 }
@@ -787,7 +763,7 @@ static jv_status diff_forward(DiffArgs a, const DiffPlan &plan, void *planes, hi
         constexpr bool SPLIT = decltype(split)::value;
         using Out = std::conditional_t<SPLIT, float, TO>;
         if constexpr (sizeof(T) == 2 && WAVES == 1) {
-            if (a.group * (long long)a.n_q <= 16) {
+            if (diff_both_maps(true, a.group * (long long)a.n_q)) {
                 hipLaunchKernelGGL((diff_attn_fwd_bf16_kernel<Out, W, 1, SPLIT, true>), grid, dim3(64), 0, stream, a);
                 return;
             }

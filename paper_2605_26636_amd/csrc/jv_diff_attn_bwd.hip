@@ -855,13 +855,6 @@ __global__ void __launch_bounds__(1024) diff_attn_dlambda_kernel(DiffArgs a) {
     }
 }
 
-// Parts of the tiles that the workgroups of a pass are cut into where they do not fill the chip (512 of bf16 tensors at a time, 256 of fp32
-// ones): as many as fill it, twice that where a causal mask makes some much longer than others; of four tiles at least, of two of fp32
-// tensors, 16 at most.
-static int diff_bwd_parts(long long items, long long tiles, bool bf16, bool causal) {
-    const long long holds = (bf16 ? 512 : 256) * (causal ? 2 : 1);
-    return (int)std::max(1ll, std::min({holds / items, tiles / (bf16 ? 4 : 2), 16ll}));
-}
 struct DiffBwdPlan {
     int q_blocks, k_blocks, q_parts, k_parts;
     size_t stats, lam, dq, dkv, planes;  // bytes of the workspace's pieces, in this order

@@ -5,6 +5,7 @@
 // Bound by memory where rows are many.
 #include "jv_common.h"
 #include "jv_mfma.h"
+#include "jv_plan.h"
 
 #include <type_traits>
 
@@ -19,10 +20,6 @@ struct NormGradArgs {
     int cols;
     float eps;
 };
-
-// Workgroups of a launch at most (each leaves column sums to be added), and their threads.  32 768 x 1024 in bf16 with a residual 50 us with 1 024
-// of 256 threads, 46 with these: half the sums.
-constexpr int kNormGradMostGroups = 512, kNormGradThreads = 512;
 
 // Eight columns from an element on.
 template <bool BF16>
@@ -227,33 +224,22 @@ __global__ void __launch_bounds__(1024) layernorm_bwd_columns_kernel(const float
     else dbeta[c - cols] = sum;
 }
 
-// Lanes a row takes and pieces a lane, f(integral_constant LANES, integral_constant NV).
+// f(integral_constant LANES, integral_constant NV) for rows of `cols`.
 template <typename F>
 static void norm_with_row(int cols, F f) {
-    const int pieces = cols / 8;
-    using One = std::integral_constant<int, 1>;
-    using Two = std::integral_constant<int, 2>;
-    if (pieces <= 8) f(std::integral_constant<int, 8>(), One());
-    else if (pieces <= 16) f(std::integral_constant<int, 16>(), One());
-    else if (pieces <= 32) f(std::integral_constant<int, 32>(), One());
-    else if (pieces <= 64) f(std::integral_constant<int, 64>(), One());
-    else if (pieces <= 128) f(std::integral_constant<int, 64>(), Two());
-    else if (pieces <= 256) f(std::integral_constant<int, 128>(), Two());
-    else if (pieces <= 512) f(std::integral_constant<int, 256>(), Two());
-    else f(std::integral_constant<int, 512>(), Two());
-}
-
-// Workgroups: one a step of rows up to 256 (one a unit), then two steps each, 256 up to 1 024 steps, above that 512: every workgroup's column sums
-// are written and read again, which more of them must earn.  256 / 512 workgroups, us, in bf16 with a residual: 1 000 x 8192 (1 000
-// steps) 33 / 41, 6 000 x 1024 (750) 17.3 / 17.3 (without residual 13.2 / 15.7), 5 000 x 1280 (1 250) 28.1 / 23.2, 16 000 x 2048 (4 000) 84 / 59.
-static long long norm_groups(long long rows, int cols) {
-    long long steps = 0;
-    norm_with_row(cols, [&](auto lanes, auto) {
-        constexpr int per = kNormGradThreads / decltype(lanes)::value;
-        steps = (rows + per - 1) / per;
-    });
-    if (steps <= 256) return steps;
-    return steps <= 512 ? (steps + 1) / 2 : steps <= 1024 ? 256 : kNormGradMostGroups;
+    auto lanes = [&](auto l) {
+        if (norm_grad_pieces(cols) == 1) f(l, std::integral_constant<int, 1>());
+        else f(l, std::integral_constant<int, 2>());
+    };
+    switch (norm_grad_lanes(cols)) {
+        case 8: return f(std::integral_constant<int, 8>(), std::integral_constant<int, 1>());
+        case 16: return f(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
+        case 32: return f(std::integral_constant<int, 32>(), std::integral_constant<int, 1>());
+        case 64: return lanes(std::integral_constant<int, 64>());
+        case 128: return f(std::integral_constant<int, 128>(), std::integral_constant<int, 2>());
+        case 256: return f(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
+        default: return f(std::integral_constant<int, 512>(), std::integral_constant<int, 2>());
+    }
 }
 
 static jv_status norm_check_sizes(int64_t rows, int32_t cols) {
@@ -271,7 +257,7 @@ extern "C" {
 size_t jv_layernorm_bwd_workspace_bytes(int64_t rows, int32_t cols) {
     jv::clear_error();
     if (jv::norm_check_sizes(rows, cols) != JV_OK) return 0;
-    return ((size_t)jv::norm_groups(rows, cols) * 2 * cols * 4 + 255) & ~(size_t)255;
+    return ((size_t)jv::norm_grad_groups(rows, cols) * 2 * cols * 4 + 255) & ~(size_t)255;
 }
 
 jv_status jv_layernorm_bwd(const void *x, const float *gamma, const void *dy, const void *residual, void *dx,
@@ -301,7 +287,7 @@ jv_status jv_layernorm_bwd(const void *x, const float *gamma, const void *dy, co
     }
     const jv::NormGradArgs a{x, dy, residual, gamma, dx, dgamma ? (float *)workspace : nullptr, rows, cols, eps};
     const hipStream_t stream = (hipStream_t)hip_stream;
-    const int groups = (int)jv::norm_groups(rows, cols);
+    const int groups = (int)jv::norm_grad_groups(rows, cols);
     jv::norm_with_row(cols, [&](auto lanes, auto nv) {
         constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value;
         auto kernel = x_dtype == JV_BF16 ? (dy_dtype == JV_BF16 ? jv::layernorm_bwd_kernel<true, true, L, NV> : jv::layernorm_bwd_kernel<true, false, L, NV>)

@@ -187,4 +187,57 @@ constexpr bool prefix_in_chains_wide(int keys, int queries, int bh) {
     return stages > kPrefixChainsWide && blocks * (96 + queries) <= 96 * line && prefix_rows_fit(keys, queries, kPrefixChainsWide);
 }
 
+// Differential attention.
+constexpr int kDiffTile = 32;  // tokens of a tile
+constexpr long long diff_min(long long x, long long y) { return x < y ? x : y; }
+constexpr long long diff_max(long long x, long long y) { return x > y ? x : y; }
+// Up to 16 rows of bf16 tensors (queries, all heads of a group together) a wavefront holds twice, once for each map.
+constexpr bool diff_both_maps(bool bf16, long long n_rows) { return bf16 && n_rows <= 16; }
+// How a forward pass is cut: wavefronts a workgroup (32 rows each) and parts of the keys.  Up to 64 rows (a few queries, all heads
+// of a group together) take one wavefront each; more take workgroups of four, which share the tiles.  Keys are cut where
+// the launch would leave units idle: into as many parts as the chip holds workgroups at a time (single wavefronts: three or six a unit, as their
+// LDS lets; one query token against 16 384 keys x 8 sequences 53 us in 2 048 of them, 41 in 768), at most 64 (a wavefront of
+// the join holds one part a lane).  Two and four tiles at least, us: one query against 2 x 1 374 keys x 16 heads 11.3 / 12.3, against 300 x 8 11.0 / 14.4, against
+// 4 x 4 096 x 16 19.6 / 18.7 (48 and 32 parts), 40 queries against 2 x 1 024 x 8 14.2 / 12.1, 577 tokens x 8 25.8 / 24.3.
+struct DiffPlan {
+    int waves, blocks, splits, tiles_per_split;
+};
+constexpr DiffPlan diff_plan(int B, int kv_heads, long long n_rows, int n_k, int W, bool bf16) {
+    const int waves = n_rows <= 64 ? 1 : 4, blocks = (int)((n_rows + 32 * waves - 1) / (32 * waves));
+    const long long groups = (long long)B * kv_heads * blocks, tiles = (n_k + kDiffTile - 1) / kDiffTile;
+    const long long holds = waves == 1 ? (bf16 || W == 128 ? 768 : 1536) : bf16 ? 512 : 256;
+    // tiles of a part: four of bf16 tensors (of few rows two, up to 24 parts), one of fp32 ones, whose tiles take 2 us and more
+    const long long most = !bf16 ? tiles : diff_both_maps(bf16, n_rows) ? diff_max(tiles / 4, diff_min(tiles / 2, 24)) : tiles / 4;
+    const long long splits = diff_max(1, diff_min(diff_min(groups * 2 > holds ? 1 : holds / groups, most), 64));
+    const int per_split = (int)((tiles + splits - 1) / splits);
+    return {waves, blocks, (int)((tiles + per_split - 1) / per_split), per_split};
+}
+// Parts of the tiles that the workgroups of a pass are cut into where they do not fill the chip (512 of bf16 tensors at a time, 256 of fp32
+// ones): as many as fill it, twice that where a causal mask makes some much longer than others; of four tiles at least, of two of fp32
+// tensors, 16 at most.
+constexpr int diff_bwd_parts(long long items, long long tiles, bool bf16, bool causal) {
+    const long long holds = (bf16 ? 512 : 256) * (causal ? 2 : 1);
+    return (int)diff_max(1, diff_min(diff_min(holds / items, tiles / (bf16 ? 4 : 2)), 16));
+}
+
+// LayerNorm's gradient: lanes a row of `cols` (a multiple of 8, up to 8192) takes, and pieces of eight columns a lane.
+constexpr int norm_grad_lanes(int cols) {
+    int lanes = 8;
+    while (lanes < 64 && 8 * lanes < cols) lanes *= 2;
+    while (16 * lanes < cols) lanes *= 2;
+    return lanes;
+}
+constexpr int norm_grad_pieces(int cols) { return 8 * norm_grad_lanes(cols) < cols ? 2 : 1; }
+// Workgroups of a launch at most (each leaves column sums to be added), and their threads.  32 768 x 1024 in bf16 with a residual 50 us with 1 024
+// of 256 threads, 46 with these: half the sums.
+constexpr int kNormGradMostGroups = 512, kNormGradThreads = 512;
+// Workgroups: one a step of rows up to 256 (one a unit), then two steps each, 256 up to 1 024 steps, above that 512: every workgroup's column sums
+// are written and read again, which more of them must earn.  256 / 512 workgroups, us, in bf16 with a residual: 1 000 x 8192 (1 000
+// steps) 33 / 41, 6 000 x 1024 (750) 17.3 / 17.3 (without residual 13.2 / 15.7), 5 000 x 1280 (1 250) 28.1 / 23.2, 16 000 x 2048 (4 000) 84 / 59.
+constexpr long long norm_grad_groups(long long rows, int cols) {
+    const long long per = kNormGradThreads / norm_grad_lanes(cols), steps = (rows + per - 1) / per;
+    if (steps <= 256) return steps;
+    return steps <= 512 ? (steps + 1) / 2 : steps <= 1024 ? 256 : kNormGradMostGroups;
+}
+
 }  // namespace jv
