@@ -33,11 +33,11 @@ struct DiffArgs {
     int splits, tiles_per_split;
     // gradient
     TensorArg d_o, dq, dk, dv;
-    float *stats;                   // [4 or 6][B * heads * n_q]: see diff_attn_rows_kernel
+    float *stats;                   // [4 or 7][B * heads * n_q]: see diff_attn_rows_kernel
     const __bf16 *planes[4];        // fp32 tensors: Q, K, V, dO split, [B * heads * n][3][W] each
     int parts;                      // of the tiles of a workgroup's rows or keys; each leaves sums of its own where there are several:
     float *dq_part, *dkv_part;      // [parts][B * heads * n_q][W]; [parts][B * kv_heads * n_k][2 W]
-    float *lam_part;                // [B * heads * row blocks * parts]: sums of P2 o dP
+    float *lam_part;                // [B * heads * row blocks * parts]: sums of P2 o dP or D2
     float *dlq1, *dlk1, *dlq2, *dlk2;
     int blocks;                     // blocks of rows (or keys) a (batch, head) has
     long long items;                // workgroups with work

@@ -15,7 +15,7 @@ namespace jv {
 //     [2]        -D1            [3]   -lambda (D1 - D2),    Dm = rowsum(dO o (Pm V)),
 // and for fp32 tensors, whose weights e inv with e = 2^(c score - m) keep the reference m and the sum 1 / inv apart (their logarithm, rounded, would
 // cost the weights 2^-24 of its size),
-//     [0], [1]   -m1, -m2;      [2], [3]   f1 = inv1, h1 = -D1 inv1;      [4], [5]   f2 = -lambda inv2, h2 = lambda D2 inv2:
+//     [0], [1]   -m1, -m2;      [2], [3]   f1 = inv1, h1 = -D1 inv1;      [4], [5]   f2 = -lambda inv2, h2 = lambda D2 inv2;      [6]   D2:
 // dS1 = e1 (f1 dP + h1), dS2 = e2 (f2 dP + h2), P1 - lambda P2 = e1 f1 + e2 f2.
 // A row takes as many lanes as it has 16-byte pieces.
 template <typename T, int W>
@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(256) diff_attn_rows_kernel(DiffArgs a) {
         d1 += __shfl_xor(d1, x);
         d2 += __shfl_xor(d2, x);
     }
-    constexpr int STATS = sizeof(T) == 2 ? 4 : 6;
+    constexpr int STATS = sizeof(T) == 2 ? 4 : 7;
     if (!live || ch >= STATS * PER) return;
     const long long n = diff_rows(a);
     const int which = ch / PER;  // a statistic a lane
@@ -73,6 +73,8 @@ __global__ void __launch_bounds__(256) diff_attn_rows_kernel(DiffArgs a) {
         stat = which < 2 ? -INFINITY : 0.f;
     } else if (which < 2) {
         stat = -a.ml[2 * which * n + row];
+    } else if (which == 6) {
+        stat = d2;
     } else {
         const float inv = 1.f / a.ml[(which < 4 ? 1 : 3) * n + row];
         stat = inv * (which == 2 ? 1.f : which == 3 ? -d1 : which == 4 ? -lam : lam * d2);
@@ -89,7 +91,9 @@ __device__ inline void diff_part(const DiffArgs &a, int part, int total, int *fr
 // What the query pass knows of a query: its weights are e inv with e = 2^(c score - m), and the gradients of its logits
 // dS1 = e1 (dP f1 + h1), dS2 = e2 (dP f2 + h2).
 struct DiffRowGrad {
-    float minus_m1, minus_m2, f1, h1, f2, h2, inv2;
+    float minus_m1, minus_m2, f1, h1, f2, h2;
+    float inv2;  // bf16 tensors
+    float d2;    // fp32 tensors
     __device__ void load(const DiffArgs &a, long long row, bool sees, float lam) {
         minus_m1 = minus_m2 = -INFINITY;
         f1 = h1 = f2 = h2 = inv2 = 0.f;
@@ -106,7 +110,7 @@ struct DiffRowGrad {
     }
     __device__ void load_f32(const DiffArgs &a, long long row, bool sees) {
         minus_m1 = minus_m2 = -INFINITY;
-        f1 = h1 = f2 = h2 = inv2 = 0.f;
+        f1 = h1 = f2 = h2 = d2 = 0.f;
         if (!sees) return;
         const long long n = diff_rows(a);
         const float *stat = a.stats + row;
@@ -116,7 +120,7 @@ struct DiffRowGrad {
         h1 = stat[3 * n];
         f2 = stat[4 * n];
         h2 = stat[5 * n];
-        inv2 = 1.f / a.ml[3 * n + row];
+        d2 = stat[6 * n];
     }
 };
 
@@ -181,11 +185,14 @@ struct DiffQueries {
 };
 
 // Scores and dP of a tile (rows: keys) become the gradients of the logits, in place.
+// For lambda, bf16 tensors add up e2 dP here: their D2 holds the rounding of P2 V's weights and rows, which shows in a sum of so many signs.  fp32
+// tensors add up D2 (diff_attn_dq_f32_kernel).
+template <bool LAMBDA>
 __device__ inline void diff_logit_grads(f32x16 &s1, f32x16 &s2, const f32x16 &dp, const DiffRowGrad &r, float c, float &lam_sum) {
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
         const float e1 = __builtin_amdgcn_exp2f(fmaf(s1[v], c, r.minus_m1)), e2 = __builtin_amdgcn_exp2f(fmaf(s2[v], c, r.minus_m2));
-        lam_sum = fmaf(e2, dp[v], lam_sum);
+        if (LAMBDA) lam_sum = fmaf(e2, dp[v], lam_sum);
         s1[v] = e1 * fmaf(dp[v], r.f1, r.h1);
         s2[v] = e2 * fmaf(dp[v], r.f2, r.h2);
     }
@@ -269,7 +276,7 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dq_bf16_kernel(DiffArgs a) {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) dp = mfma32(as_bf16x8(y[ks]), go[KS + ks], dp);
         if ((tile + 1) * kDiffTile > p.least) diff_hide_keys(s1, s2, tile * kDiffTile, p.limit > 0 ? p.limit : a.n_k + kDiffTile, g);
-        diff_logit_grads(s1, s2, dp, r, a.c, lam_sum);
+        diff_logit_grads<true>(s1, s2, dp, r, a.c, lam_sum);
         bf16x8 ds1[2], ds2[2];
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
@@ -292,7 +299,8 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dq_bf16_kernel(DiffArgs a) {
     diff_finish_dq<__bf16, W>(a, acc, lam_sum * r.inv2, p.b, p.h, p.block, p.part, wave_lam, tid);
 }
 
-// The same for fp32 tensors, on operands of three bf16 numbers.
+// The same for fp32 tensors, on operands of three bf16 numbers.  For lambda D2 is added up, once a row: the matrix unit's dP, a sum of so many small
+// terms, lies a little low whatever its sign (1e-8 of its size), and Sum P2 o dP, where signs cancel, was 1e-4 off at 4 096 tokens through it.
 template <int W>
 __global__ void __launch_bounds__(256, 1) diff_attn_dq_f32_kernel(DiffArgs a) {
     using Lds = DiffLds<W>;
@@ -327,11 +335,10 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dq_f32_kernel(DiffArgs a) {
 #pragma unroll
     for (int ks = 0; ks < 2 * KS; ++ks)  // (waited for here, not inside the loop)
         asm volatile("" : "+v"(q[ks].x[0]), "+v"(q[ks].x[1]), "+v"(q[ks].x[2]), "+v"(go[ks].x[0]), "+v"(go[ks].x[1]), "+v"(go[ks].x[2]));
-    asm volatile("" : "+v"(r.minus_m1), "+v"(r.minus_m2), "+v"(r.f1), "+v"(r.h1), "+v"(r.f2), "+v"(r.h2), "+v"(r.inv2));
+    asm volatile("" : "+v"(r.minus_m1), "+v"(r.minus_m2), "+v"(r.f1), "+v"(r.h1), "+v"(r.f2), "+v"(r.h2), "+v"(r.d2));
     f32x16 acc[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) diff_zero(acc[cb]);
-    float lam_sum = 0.f;
     const unsigned rows0 = Lds::rows(lds_address(smem), lane), cols0 = Lds::cols(lds_address(smem), lane);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     lds_barrier();
@@ -363,7 +370,8 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dq_f32_kernel(DiffArgs a) {
         diff_read_cols3<W, 0, 0>(v[0], cols, 0);
         __builtin_amdgcn_sched_barrier(0);
         if ((tile + 1) * kDiffTile > p.least) diff_hide_keys(s1, s2, tile * kDiffTile, p.limit > 0 ? p.limit : a.n_k + kDiffTile, g);
-        diff_logit_grads(s1, s2, dp, r, a.c, lam_sum);
+        float none = 0.f;
+        diff_logit_grads<false>(s1, s2, dp, r, a.c, none);
         diff_landed(v[0]);
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
@@ -383,7 +391,7 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dq_f32_kernel(DiffArgs a) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the next tile, for every wavefront, and every wavefront done with this one
         lds_barrier();
     }
-    diff_finish_dq<float, W>(a, acc, lam_sum * r.inv2, p.b, p.h, p.block, p.part, wave_lam, tid);
+    diff_finish_dq<float, W>(a, acc, p.part == 0 && g == 0 ? r.d2 : 0.f, p.b, p.h, p.block, p.part, wave_lam, tid);
 }
 
 // Where a workgroup of the key pass stands: 128 keys of a kv head; the tiles of its group's heads, one head after the other, of
@@ -867,7 +875,7 @@ static DiffBwdPlan diff_bwd_plan(const jv_diff_attn_desc *d) {
     p.q_parts = diff_bwd_parts((long long)d->batch * d->heads * p.q_blocks, (d->n_k + kDiffTile - 1) / kDiffTile, d->dtype == JV_BF16, d->causal);
     p.k_parts = diff_bwd_parts((long long)d->batch * d->kv_heads * p.k_blocks, (d->n_q + kDiffTile - 1) / kDiffTile * group, d->dtype == JV_BF16, d->causal);
     auto whole = [](long long bytes) { return ((size_t)bytes + 255) & ~(size_t)255; };
-    p.stats = whole(rows * (d->dtype == JV_BF16 ? 16 : 24));
+    p.stats = whole(rows * (d->dtype == JV_BF16 ? 16 : 28));
     p.planes = diff_planes_bytes(d, true);
     p.lam = whole((long long)d->batch * d->heads * p.q_blocks * p.q_parts * 4);
     p.dq = p.q_parts > 1 ? whole(rows * p.q_parts * d->head_dim * 4) : 0;

@@ -36,6 +36,25 @@ def test_parts_of_the_gradient(dtype, W, B, H, G, n_q, n_k, causal):
     D.Bounds(x, dtype, causal=causal, backward=True).check(D.run(x, causal=causal, backward=True))
 
 
+@pytest.mark.parametrize("dtype,W", [("bf16", 64), ("bf16", 128), ("fp32", 64), ("fp32", 128)])
+def test_lambda_s_gradient_is_not_biased(dtype, W):
+    """dlambda_h = -Sum P2 o dP sums numbers of both signs.  Errors of its terms, at most 8 half steps of fp32 each (score, exponential, dP, sum),
+    and of its rows (reference, denominator), as many, that do not know of each other add up like a random walk: six standard deviations."""
+    B, H, N = 2, 6, 2600
+    x = D.make(25, B, H, H, N, N, W, dtype, per_head=True)
+    out = D.run(x, backward=True)
+    q, k, v, d_o = (x[n].double().cuda() for n in ("q", "k", "v", "d_o"))
+    lam = [t.double().cuda() for t in x["lam"]]
+    d = W // 2
+    terms = (torch.matmul(q[..., d:], k[..., d:].transpose(-1, -2)) / d ** 0.5).softmax(-1) * torch.matmul(d_o, v.transpose(-1, -2))
+    rows = terms.sum(-1)
+    far = 6 * 8 * D.EPS * ((terms * terms).sum((0, 2, 3)).sqrt() + (rows * rows).sum((0, 2)).sqrt())
+    want = rows.sum((0, 2)) * (lam[2] * lam[3]).sum(-1).exp()
+    far = far * (lam[2] * lam[3]).sum(-1).exp() + 8 * D.EPS * want.abs()
+    got = (out["lam"][3].double() * lam[2]).sum(-1) / (lam[2] * lam[2]).sum(-1)   # d_k2 = -dlambda e2 q2
+    D.Bounds.one("dlambda", got.cpu().numpy(), want.cpu().numpy(), far.cpu().numpy())
+
+
 @pytest.mark.parametrize("size", [1e-12, 1e12])
 def test_fp32_numbers_far_from_one(size):
     """Each number goes into its products as a sum of three of bf16, whatever its exponent: relative errors stay those of numbers near one."""
