@@ -258,7 +258,7 @@ __device__ inline void diff_softmax_pack(DiffMap<W> &w, DiffWeights<TERMS> &p, c
 // channels, so that a tile takes one block of scores, one softmax and half the products with V.  There is time for weights of
 // two terms then.
 template <typename TO, int W, int WAVES, bool SPLIT, bool BOTH = false>
-__global__ void __launch_bounds__(64 * WAVES, 2) diff_attn_fwd_bf16_kernel(DiffArgs a) {
+__global__ void __launch_bounds__(64 * WAVES, W == 128 && WAVES == 1 ? 1 : 2) diff_attn_fwd_bf16_kernel(DiffArgs a) {
     static_assert(!BOTH || WAVES == 1, "a wavefront holds all rows twice");
     using Lds = DiffLds<W>;
     constexpr int KS = W / 32, CB = W / 32, TILE = kDiffTile * 2 * W, STAGE = 2 * TILE, RING = 3;  // a stage: K rows, then V rows
@@ -588,8 +588,8 @@ __global__ void __launch_bounds__(256) diff_attn_join_few_kernel(DiffArgs a) {
     }
 }
 
-// More parts, up to 64: a workgroup a row, whose four wavefronts take every fourth part each, eight parts' loads at a time (one query token
-// against 16 384 keys x 8 sequences x 16 heads in 24 parts 6 us; in 39 by one wavefront, one part after the other, 21).
+// More parts, up to 64: a workgroup a row, whose four wavefronts take every fourth part each, eight parts' loads at a time (one query
+// against 8 192 keys x 8 heads of 128 in 64 parts, both kernels: 22.0 us with one part's loads after the other's, 17.9 so).
 template <typename T, typename TO, int W>
 __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -610,14 +610,22 @@ __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
     constexpr int PER = W / 32;  // channels a lane: lanes 0 .. 31 those of the first map, 32 .. 63 of the second
     float x[PER] = {};
     const float *part = a.part + at * (2 * W + 4) + 4 + lane * PER;
-#pragma unroll 8
-    for (int s = wave; s < a.splits; s += 4) {
-        float y[PER];
+    for (int first = wave; first < a.splits; first += 32) {
+        float y[8][PER];
 #pragma unroll
-        for (int e = 0; e < PER; ++e) y[e] = part[s * all * (2 * W + 4) + e];
-        const float f_first = __shfl(f1, s), f_second = __shfl(f2, s), f = lane < 32 ? f_first : f_second;
+        for (int i = 0; i < 8; ++i) {
+            const long long s = min(first + 4 * i, a.splits - 1);
 #pragma unroll
-        for (int e = 0; e < PER; ++e) x[e] = seen >> s & 1 ? fmaf(y[e], f, x[e]) : x[e];
+            for (int e = 0; e < PER; ++e) y[i][e] = part[s * all * (2 * W + 4) + e];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int s = first + 4 * i;
+            const float f_first = __shfl(f1, s & 63), f_second = __shfl(f2, s & 63), f = lane < 32 ? f_first : f_second;
+            const bool taken = s < a.splits && (seen >> (s & 63) & 1);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) x[e] = taken ? fmaf(y[i][e], f, x[e]) : x[e];
+        }
     }
 #pragma unroll
     for (int e = 0; e < PER; ++e) sums[wave][lane * PER + e] = x[e];
