@@ -588,25 +588,43 @@ __global__ void __launch_bounds__(256) diff_attn_join_few_kernel(DiffArgs a) {
     }
 }
 
-// More parts, up to 64: a workgroup a row, whose four wavefronts take every fourth part each, eight parts' loads at a time (one query
-// against 8 192 keys x 8 heads of 128 in 64 parts, both kernels: 22.0 us with one part's loads after the other's, 17.9 so).
+// More parts, up to kDiffMostParts: a workgroup a row. A thread holds a part's references and sums; then its four wavefronts take every fourth part
+// each, eight parts' loads at a time (one query against 8 192 keys x 8 heads of 128 in 64 parts, both kernels: 22.0 us with one part's
+// loads after the other's, 17.9 so).
 template <typename T, typename TO, int W>
 __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
+    static_assert(kDiffMostParts <= 256, "a part a thread");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long long all = diff_rows(a), at = blockIdx.x;
-    __shared__ float sums[4][2 * W];
+    __shared__ float sums[4][2 * W], top[2][4], total[2][4], factor[2][256];
     const DiffRowPlace place(a, at);
     f32x4 ml = {-INFINITY, 0.f, -INFINITY, 0.f};
-    if (lane < a.splits) ml = *(const f32x4 *)(a.part + ((long long)lane * all + at) * (2 * W + 4));
+    if ((int)threadIdx.x < a.splits) ml = *(const f32x4 *)(a.part + ((long long)threadIdx.x * all + at) * (2 * W + 4));
     float m1 = ml[0], m2 = ml[2];
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) {
         m1 = fmaxf(m1, __shfl_xor(m1, x));
         m2 = fmaxf(m2, __shfl_xor(m2, x));
     }
-    const float f1 = ml[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m1), f2 = ml[2] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[2] - m2);
-    const float l1 = wave_sum(ml[1] * f1), l2 = wave_sum(ml[3] * f2);
-    const unsigned long long seen = __builtin_amdgcn_ballot_w64(ml[0] != -INFINITY);
+    if (lane == 0) {
+        top[0][wave] = m1;
+        top[1][wave] = m2;
+    }
+    __syncthreads();
+    m1 = fmaxf(fmaxf(top[0][0], top[0][1]), fmaxf(top[0][2], top[0][3]));
+    m2 = fmaxf(fmaxf(top[1][0], top[1][1]), fmaxf(top[1][2], top[1][3]));
+    const bool sees = ml[0] != -INFINITY;  // (both maps see the same keys; the sums of a part that sees none were not written)
+    const float f1 = sees ? __builtin_amdgcn_exp2f(ml[0] - m1) : 0.f, f2 = sees ? __builtin_amdgcn_exp2f(ml[2] - m2) : 0.f;
+    float l1 = wave_sum(ml[1] * f1), l2 = wave_sum(ml[3] * f2);
+    factor[0][threadIdx.x] = sees ? f1 : -1.f;
+    factor[1][threadIdx.x] = sees ? f2 : -1.f;
+    if (lane == 0) {
+        total[0][wave] = l1;
+        total[1][wave] = l2;
+    }
+    __syncthreads();
+    l1 = (total[0][0] + total[0][1]) + (total[0][2] + total[0][3]);
+    l2 = (total[1][0] + total[1][1]) + (total[1][2] + total[1][3]);
     constexpr int PER = W / 32;  // channels a lane: lanes 0 .. 31 those of the first map, 32 .. 63 of the second
     float x[PER] = {};
     const float *part = a.part + at * (2 * W + 4) + 4 + lane * PER;
@@ -621,10 +639,9 @@ __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int s = first + 4 * i;
-            const float f_first = __shfl(f1, s & 63), f_second = __shfl(f2, s & 63), f = lane < 32 ? f_first : f_second;
-            const bool taken = s < a.splits && (seen >> (s & 63) & 1);
+            const float f = s < a.splits ? factor[lane >> 5][s] : -1.f;
 #pragma unroll
-            for (int e = 0; e < PER; ++e) x[e] = taken ? fmaf(y[i][e], f, x[e]) : x[e];
+            for (int e = 0; e < PER; ++e) x[e] = f >= 0.f ? fmaf(y[i][e], f, x[e]) : x[e];
         }
     }
 #pragma unroll

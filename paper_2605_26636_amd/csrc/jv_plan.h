@@ -196,9 +196,10 @@ constexpr bool diff_both_maps(bool bf16, long long n_rows) { return bf16 && n_ro
 // How a forward pass is cut: wavefronts a workgroup (32 rows each) and parts of the keys.  Up to 64 rows (a few queries, all heads
 // of a group together) take one wavefront each; more take workgroups of four, which share the tiles.  Keys are cut where
 // the launch would leave units idle: into as many parts as the chip holds workgroups at a time (single wavefronts: three or six a unit, as their
-// LDS lets; one query token against 16 384 keys x 8 sequences 53 us in 2 048 of them, 41 in 768), at most 64 (a wavefront of
-// the join holds one part a lane).  Two and four tiles at least, us: one query against 2 x 1 374 keys x 16 heads 11.3 / 12.3, against 300 x 8 11.0 / 14.4, against
+// LDS lets; one query token against 16 384 keys x 8 sequences 53 us in 2 048 of them, 41 in 768), at most 256
+// (64 / 256, us: one query against 65 536 keys of 128 x 2 heads 48.3 / 25.6, 32 768 x 4 of 64 21.1 / 17.5, 8 192 fp32 keys x 2 25.2 / 21.7).  Two and four tiles at least, us: one query against 2 x 1 374 keys x 16 heads 11.3 / 12.3, against 300 x 8 11.0 / 14.4, against
 // 4 x 4 096 x 16 19.6 / 18.7 (48 and 32 parts), 40 queries against 2 x 1 024 x 8 14.2 / 12.1, 577 tokens x 8 25.8 / 24.3.
+constexpr int kDiffMostParts = 256;
 struct DiffPlan {
     int waves, blocks, splits, tiles_per_split;
 };
@@ -208,7 +209,7 @@ constexpr DiffPlan diff_plan(int B, int kv_heads, long long n_rows, int n_k, int
     const long long holds = waves == 1 ? (bf16 || W == 128 ? 768 : 1536) : bf16 ? 512 : 256;
     // tiles of a part: four of bf16 tensors (of few rows two, up to 24 parts), one of fp32 ones, whose tiles take 2 us and more
     const long long most = !bf16 ? tiles : diff_both_maps(bf16, n_rows) ? diff_max(tiles / 4, diff_min(tiles / 2, 24)) : tiles / 4;
-    const long long splits = diff_max(1, diff_min(diff_min(groups * 2 > holds ? 1 : holds / groups, most), 64));
+    const long long splits = diff_max(1, diff_min(diff_min(groups * 2 > holds ? 1 : holds / groups, most), kDiffMostParts));
     const int per_split = (int)((tiles + splits - 1) / splits);
     return {waves, blocks, (int)((tiles + per_split - 1) / per_split), per_split};
 }

@@ -12,7 +12,7 @@ from paper_2605_26636_amd import binding
 pytestmark = pytest.mark.gpu
 
 ROWS = [(2, 8), (1, 17), (4, 16), (5, 13)]   # heads of one kv head, queries: 16, 17, 64, 65 rows
-KEYS = [20, 50, 70, 140, 200, 270, 330, 530, 900, 1540, 2040, 8190]
+KEYS = [20, 50, 70, 140, 200, 270, 330, 530, 900, 1540, 2040, 8190, 33000]
 # B, heads, kv_heads, n_q, n_k, causal
 GRADIENTS = [(1, 2, 1, 150, 2100, False), (1, 1, 1, 2100, 150, False), (1, 2, 2, 1100, 1100, True), (2, 2, 1, 300, 260, True), (3, 4, 4, 200, 200, False),
              (2, 1, 1, 50, 45, True)]

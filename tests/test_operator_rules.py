@@ -25,7 +25,7 @@ def test_plans_of_the_forward_pass(rule):  # noqa: F811
         tiles, groups = (n_k + 31) // 32, B * G * blocks
         assert waves == (1 if rows <= 64 else 4) and 32 * waves * (blocks - 1) < rows <= 32 * waves * blocks
         # no part without a tile, none missing, and no more than a launch or the join takes
-        assert 1 <= splits <= 64 and per * splits >= tiles and per * (splits - 1) < tiles
+        assert 1 <= splits <= 256 and per * splits >= tiles and per * (splits - 1) < tiles
         holds = 768 if waves == 1 and (bf16 or W == 128) else 1536 if waves == 1 else 512 if bf16 else 256
         assert splits == 1 or groups * splits <= holds
         assert not bf16 or splits == 1 or per >= (2 if rows <= 16 else 4)
@@ -33,7 +33,7 @@ def test_plans_of_the_forward_pass(rule):  # noqa: F811
 
 def test_the_gpu_tests_reach_every_join(rule):  # noqa: F811
     def kind(splits):
-        return 1 if splits == 1 else 2 if splits == 2 else 4 if splits <= 4 else 8 if splits <= 8 else 9 if splits < 64 else 64
+        return 1 if splits == 1 else 2 if splits == 2 else 4 if splits <= 4 else 8 if splits <= 8 else 9 if splits <= 32 else 33 if splits <= 64 else 65
     for bf16 in (False, True):
         for W in (64, 128):
             cases = [(1, 1, h * n, n_k, W, bf16) for h, n in V.ROWS for n_k in V.KEYS]
@@ -41,7 +41,7 @@ def test_the_gpu_tests_reach_every_join(rule):  # noqa: F811
             for c, (waves, _, splits, _) in zip(cases, plan(rule, cases)):
                 kinds.setdefault((waves, bf16 and c[2] <= 16), set()).add(kind(splits))
             assert set(kinds) == ({(1, True), (1, False), (4, False)} if bf16 else {(1, False), (4, False)})
-            assert all(k == {1, 2, 4, 8, 9, 64} for k in kinds.values()), (bf16, W, kinds)
+            assert all(k == {1, 2, 4, 8, 9, 33, 65} for k in kinds.values()), (bf16, W, kinds)
 
 
 def test_parts_of_the_gradient(rule):  # noqa: F811
