@@ -487,7 +487,7 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dkv_bf16_kernel(DiffArgs a) 
     DiffKeys p;
     if (!p.find(a, wave, lane)) return;  // whole workgroup
     unsigned char *vt = smem + 2 * STAGE + wave * TILE;  // the wavefront's own values
-    DiffDma<W, 4> qload, gload;
+    DiffDma<W, 4, W == 64> qload, gload;
     int next_tile = p.tile_begin, next_head = p.kv * a.group;
     if (p.n_tiles) {
         next_head += p.from / p.n_tiles;
