@@ -234,6 +234,7 @@ __device__ inline DiffPlanes diff_global_planes(const __bf16 *row, int ks, int g
     return {{diff_global_frag(row, ks, g, live), diff_global_frag(row + W, ks, g, live), diff_global_frag(row + 2 * W, ks, g, live)}};
 }
 __device__ inline void diff_landed(u32x4 (&x)[3]) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2])); }
+__device__ inline void diff_landed(u32x4 (&x)[3], u32x4 &y) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(y)); }
 __device__ inline void diff_landed(u32x2 (&x)[6]) {
     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]));
 }
@@ -308,14 +309,14 @@ struct DiffDma {
 };
 
 // The same for the three planes of split fp32 rows.
-template <int W, int WAVES>
+template <int W, int WAVES, bool HELD = true>
 struct DiffDma3 {
-    DiffDma<W, WAVES> one;
+    DiffDma<W, WAVES, HELD> one;
     __device__ void start(const __bf16 *planes, long long row, int wave, int lane) { one.start(planes, row * 3 * W, 3 * W, wave, lane); }
     __device__ void issue(unsigned char *tiles, int row0, int limit, int wave, int lane) const {
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
-            DiffDma<W, WAVES> plane = one;
+            DiffDma<W, WAVES, HELD> plane = one;
             plane.base += p * 2 * W;
             plane.issue(tiles + p * DiffTile<W>::kBytes, row0, limit, wave, lane);
         }

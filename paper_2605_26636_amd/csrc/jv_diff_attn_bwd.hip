@@ -646,13 +646,15 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dkv_bf16_kernel(DiffArgs a) 
     diff_finish_dkv<__bf16, W>(a, dk, dv, p, g);
 }
 
-// The same for fp32 tensors, on operands of three bf16 numbers: K and V both in registers, one wavefront a SIMD.
+// The same for fp32 tensors, on operands of three bf16 numbers: K and V in registers, but for the last plane of V in rows of 128, which
+// lies in LDS; one wavefront a SIMD.
 template <int W>
 __global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
     using Lds = DiffLds<W>;
     constexpr int KS = W / 32, CB = W / 32, TILE = DiffTile<W>::kBytes, STATS = 6 * kDiffTile * 4, STAGE = 6 * TILE + 1024;  // Q planes, dO planes, statistics
     static_assert(STATS <= 1024, "stages stay 1 KB aligned");
-    __shared__ __align__(1024) unsigned char smem[2 * STAGE];
+    constexpr bool LAST = W == 128;  // the last plane of V in LDS
+    __shared__ __align__(1024) unsigned char smem[2 * STAGE + (LAST ? 4 * TILE : 0)];
     const int tid = threadIdx.x, lane = tid & 63, g = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     DiffKeys p;
     if (!p.find(a, wave, lane)) return;  // whole workgroup
@@ -661,7 +663,7 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
         head += p.from / p.n_tiles;
         tile += p.from % p.n_tiles;
     }
-    DiffDma3<W, 4> qload, gload;
+    DiffDma3<W, 4, W == 64> qload, gload;
     int next_tile = tile, next_head = head;
     qload.start(a.planes[0], ((long long)p.b * a.heads + head) * a.n_q, wave, lane);
     gload.start(a.planes[3], ((long long)p.b * a.heads + head) * a.n_q, wave, lane);
@@ -674,8 +676,10 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
         if (wave < 3) {  // statistics 2 wave and 2 wave + 1
             const char *from = diff_uniform(a.stats + 2 * wave * diff_rows(a) + ((long long)p.b * a.heads + next_head) * a.n_q + row0);
             const long long other = diff_rows(a) * 4;
-            const unsigned at = 4 * min(lane & 31, p.len_q - 1 - row0);
-            __builtin_amdgcn_global_load_lds((diff_global_cvoid *)(from + (lane >> 5) * other + at), (diff_lds_void *)(to + 6 * TILE + wave * 256), 4, 0, 0);
+            int l = lane;
+            if (LAST) asm volatile("" : "+v"(l));  // (worked out here: kept, it would come from scratch memory)
+            const unsigned at = 4 * min(l & 31, p.len_q - 1 - row0);
+            __builtin_amdgcn_global_load_lds((diff_global_cvoid *)(from + (l >> 5) * other + at), (diff_lds_void *)(to + 6 * TILE + wave * 256), 4, 0, 0);
         }
         if (++next_tile == p.tile_begin + p.n_tiles) {
             next_tile = p.tile_begin;
@@ -684,7 +688,16 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
             gload.one.base += 6ll * W * a.n_q;
         }
     };
-    if (p.from < p.to) issue(0);
+    unsigned char *vt = smem + 2 * STAGE + wave * TILE;
+    const int key0 = p.block * 128 + wave * 32;
+    if (p.from < p.to) {
+        if (LAST && key0 < p.len_k) {
+            DiffDma<W, 1> vload;
+            vload.start(a.planes[2], (((long long)p.b * a.kv_heads + p.kv) * a.n_k * 3 + 2) * W, 3 * W, 0, lane);
+            vload.issue(vt, key0, p.len_k, 0, lane);
+        }
+        issue(0);
+    }
     DiffPlanes k[2 * KS], v[2 * KS];
     {
         const bool live = p.key < p.len_k;
@@ -696,8 +709,10 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
         }
     }
 #pragma unroll
-    for (int ks = 0; ks < 2 * KS; ++ks)  // (waited for here, not inside the loop)
-        asm volatile("" : "+v"(k[ks].x[0]), "+v"(k[ks].x[1]), "+v"(k[ks].x[2]), "+v"(v[ks].x[0]), "+v"(v[ks].x[1]), "+v"(v[ks].x[2]));
+    for (int ks = 0; ks < 2 * KS; ++ks) {  // (waited for here, not inside the loop)
+        asm volatile("" : "+v"(k[ks].x[0]), "+v"(k[ks].x[1]), "+v"(k[ks].x[2]), "+v"(v[ks].x[0]), "+v"(v[ks].x[1]));
+        if (!LAST) asm volatile("" : "+v"(v[ks].x[2]));
+    }
     f32x16 dk[CB], dv[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
@@ -705,32 +720,49 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
         diff_zero(dv[cb]);
     }
     const unsigned rows0 = Lds::rows(lds_address(smem), lane), cols0 = Lds::cols(lds_address(smem), lane), stats0 = lds_address(smem) + 6 * TILE + 16 * g;
+    const unsigned vrows = Lds::rows(lds_address(vt), lane);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     lds_barrier();
     for (int at = p.from, stage = 0; at < p.to; ++at, stage ^= 1) {
-        if (at + 1 < p.to) issue(stage ^ 1);
+        if (!LAST && at + 1 < p.to) issue(stage ^ 1);
         const unsigned rows = rows0 + stage * STAGE, cols = cols0 + stage * STAGE, stats = stats0 + stage * STAGE;
         f32x16 s1, s2, dp;
         diff_zero(s1);
         diff_zero(s2);
         diff_zero(dp);
         {
-            u32x4 x[2][3];
+            u32x4 x[2][3], last[2];
             diff_read_rows3<W, 0>(x[0], rows, 0);
             diff_landed(x[0]);
 #pragma unroll
             for (int i = 0; i < 4 * KS; ++i) {  // Q operands, then dO operands
-                if (i + 1 < 2 * KS) diff_read_rows3<W, 0>(x[(i + 1) & 1], rows, i + 1);
-                else if (i + 1 < 4 * KS) diff_read_rows3<W, 3 * TILE>(x[(i + 1) & 1], rows, i + 1 - 2 * KS);
+                const int next = (i + 1) & 1;
+                if (i + 1 < 2 * KS) diff_read_rows3<W, 0>(x[next], rows, i + 1);
+                else if (i + 1 < 4 * KS) {
+                    diff_read_rows3<W, 3 * TILE>(x[next], rows, i + 1 - 2 * KS);
+                    if (LAST) last[next] = lds_read_b128_at<0>(vrows ^ 32 * (i + 1 - 2 * KS));
+                }
                 __builtin_amdgcn_sched_barrier(0);
                 bf16x8 q[3];
                 diff_rows3(x[i & 1], q);
                 if (i < KS) s1 = diff_mma6(q, k[i < KS ? i : 0].x, s1);
                 else if (i < 2 * KS) s2 = diff_mma6(q, k[i < 2 * KS ? i : 0].x, s2);
-                else dp = diff_mma6(q, v[i < 2 * KS ? 0 : i - 2 * KS].x, dp);
-                if (i + 1 < 4 * KS) diff_landed(x[(i + 1) & 1]);
+                else {
+                    DiffPlanes &y = v[i < 2 * KS ? 0 : i - 2 * KS];
+                    if (LAST) {
+                        const bf16x8 z[3] = {y.x[0], y.x[1], as_bf16x8(last[i & 1])};
+                        dp = diff_mma6(q, z, dp);
+                    } else {
+                        dp = diff_mma6(q, y.x, dp);
+                    }
+                }
+                if (i + 1 < 4 * KS) {
+                    if (LAST && i + 1 >= 2 * KS) diff_landed(x[next], last[next]);
+                    else diff_landed(x[next]);
+                }
             }
         }
+        if (LAST && at + 1 < p.to) issue(stage ^ 1);  // (not in front of the products above: two operands of theirs come from scratch memory, for which they would wait for the tile too)
         if (p.masked(a, tile)) p.hide(a, s1, s2, tile, g);
         // four rows' statistics at a time, the next four's on their way
         {
