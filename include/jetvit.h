@@ -5,7 +5,8 @@
  * The library computes the forward pass of the three token mixers that the
  * paper's Post-Training Attention Search assigns per layer -- ReLU-kernel
  * linear attention, non-overlapping 2-D window attention, and the retained
- * full softmax attention -- on caller-owned device buffers.
+ * full softmax attention -- on caller-owned device buffers, and differential
+ * attention and LayerNorm with their gradients.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -28,11 +29,11 @@
  *    JV_BF16 tensors: full, window and linear attention (prefix tokens included) and the
  *    linear-attention block with static or squeeze-dynamic filters are built for both; the
  *    focused map, token-wise filters and JV_F32 tensors for 64 only (JV_ERR_UNSUPPORTED
- *    otherwise).
+ *    otherwise).  Differential attention takes both with either element type.
  *  - Inputs are never written.  O must not overlap Q, K or V: the byte range that O's
  *    strides span may not intersect the range of any input (JV_ERR_INVALID_ARG).
  *  - Arithmetic: JV_F32 tensors are processed in fp32 throughout, or, in softmax
- *    attention over more than 32 keys, as sums of three bf16 numbers that together hold
+ *    attention over more than 32 keys and in differential attention, as sums of three bf16 numbers that together hold
  *    all 24 bits of every operand (magnitudes below 2^-110: down to 2^-133), whatever the
  *    magnitudes of the other operands, with fp32 accumulation.  JV_BF16 tensors
  *    feed bf16 matrix instructions with fp32 accumulation; softmax,
@@ -279,16 +280,19 @@ jv_status jv_full_attn_fwd(const jv_attn_desc *desc, const void *q, const void *
  *    Numbers below 0 count as 0, above n_q or n_k as n_q or n_k.
  *  - causal != 0: query i sees keys 0 .. i + k_lengths[b] - q_lengths[b] (the last query sees all keys).
  *  - A query that sees no key has a zero row in O and in dQ.
- * head_dim is 64 or 128 for both element types, o_dtype as in jv_attn_desc; at most 2^24 queries and keys and 65535
- * batch entries times heads.  Strides as in jv_attn_desc; K and V may be broadcast (stride 0), rows of O may
- * not overlap each other.  The stride of an axis of one is ignored.  scale <= 0 or NaN selects 1/sqrt(d).
- * Arithmetic: JV_F32 on fp32 matrix instructions.  JV_BF16: the weights Pm are rounded to bf16 in front of the
- * product with V, and in the gradient P1 - lambda P2 and the gradients of the logits in front of theirs; everything else is fp32.
+ * head_dim is 64 or 128 for both element types, o_dtype as in jv_attn_desc; at most 2^24 queries and keys, 2^30 queries of the
+ * heads that share K and V, and 65535 batch entries times heads.  Strides as in jv_attn_desc, stride_n up to 2^25; K and V may
+ * be broadcast (stride 0), rows of O may not overlap each other.  The stride of an axis of one is ignored.
+ * scale <= 0 or NaN selects 1/sqrt(d); one of its own lies between 1e-30 and 1e30.
+ * Arithmetic: JV_F32 as sums of three bf16 numbers (see the conventions above); an infinity among the operands gives NaN.
+ * JV_BF16: the weights Pm are rounded to bf16 in front of the product with V (up to 16 queries of the heads that share K and V: to
+ * the sum of two bf16 numbers), and in the gradient P1 - lambda P2 and the gradients of the logits in front of theirs; everything
+ * else is fp32.
  * Device memory of a call, 256-byte aligned, sized by the queries below (0 for an invalid descriptor):
  *   workspace  scratch of the call, contents unspecified afterwards; the forward pass may be given NULL
  *              where its query says 256 (nothing is kept there then).
- *   saved      forward: NULL, or memory that receives what the backward pass needs (the denominators of both
- *              softmaxes, and P2 V in the element type).  o_dtype must be dtype then (JV_ERR_UNSUPPORTED).
+ *   saved      forward: NULL, or memory that receives what the backward pass needs (the references and
+ *              denominators of both softmaxes, and P2 V in the element type).  o_dtype must be dtype then (JV_ERR_UNSUPPORTED).
  * Outputs, `saved` and workspaces may not overlap each other or anything read.
  * ------------------------------------------------------------------------- */
 typedef struct {
@@ -323,8 +327,9 @@ jv_status jv_diff_attn_fwd(const jv_diff_attn_desc *desc, const void *q, const v
  *     dQm = scale dSm Km,   dKm = scale dSm^T Qm,   dlambda_h = - sum P2 o dP,
  * dK and dV summed over the heads that share them.  d_q1 .. d_k2 receive the gradients of lambda's vectors in fp32, in their
  * layout (summed over the heads where these share one set); all four, or none (NULL).
- * The weights are formed again from the logarithm of their denominators, in fp32: off by 2^-24 of the logit's size, so that
- * logits beyond 2^20 leave no gradient of use (the forward pass takes any that are finite).
+ * The weights are formed again: for dK and dV of JV_BF16 from the logarithm of their denominators, in fp32, off by 2^-24 of the
+ * logit's size, so that logits beyond 2^20 leave no gradient of use (the forward pass takes any that are finite).
+ * Outputs in one place (d_k = d_v, say) are not looked for: each needs memory of its own.
  * Sums have a fixed order (no atomics): the same call gives the same bits.  Rows of d_q, d_k, d_v may not overlap; d_q, d_k, d_v may be views of
  * one buffer that lie between each other's rows. */
 typedef struct {

@@ -52,7 +52,7 @@ struct DiffProblem {
 // What a workgroup works on: a block of rows (or keys) of a (batch, head) and one of `parts` parts of it.  Without a mask, contiguous
 // ranges of (batch, head)s per XCD (workgroup w runs on XCD w % 8), so that the workgroups of one share its K and V in one L2.
 // Causal: the blocks with most work of all of them first (an XCD's (batch, head)s one after the other leave its last long
-// blocks alone at the end: forward pass of 2 x 4 096 tokens x 16 heads of 128 channels 291 us, now 236; where their number is a multiple of
+// blocks alone at the end: forward pass of 2 x 4 096 tokens x 16 heads of 128 channels 291 us, so 232; where their number is a multiple of
 // 8 each stays on one XCD all the same).  False where a workgroup of the rounded-up grid has no work.
 struct DiffItem {
     int part, block, bh;

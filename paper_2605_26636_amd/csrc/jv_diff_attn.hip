@@ -3,7 +3,8 @@
 // A wavefront keeps 32 rows (queries) as columns and walks the keys in tiles of 32: scores of both maps, S^T = K Q^T with half
 // the channels each, two running softmaxes, and O1^T, O2^T += V^T P with every V operand read once for both maps.
 // The difference is formed at the end, in fp32.  24 matrix instructions of 32 x 32 x 16 a tile and wavefront (W = 128),
-// against 32 exponentials a lane.
+// against 32 exponentials a lane.  Few rows, where the keys' bytes are what counts, take one wavefront each and are cut over the keys
+// (jv_plan.h); the parts are joined by a second launch.
 #include <math.h>
 #include <stdlib.h>
 
@@ -212,6 +213,11 @@ __device__ inline int diff_tiles(const DiffArgs &a, const DiffPlace &place, cons
 // both softmaxes run; the products with V, the next 16 keys' operands and then the next tile's K operands in flight.
 // Rows behind the last key are fetched as the last one, which is masked there.  Rows that see no key go along unmasked and are
 // dropped at the end.
+// Bound by the issue of matrix and vector instructions: 8 x 4 096 tokens x 8 heads of 128 751 us (1.10 PFLOP/s), 3 x 4 096 x 16 of 64 357 us (0.87). The same
+// arithmetic on numbers that stay in LDS, without loads, barriers and LDS reads, takes 83 and 85 % of that, and its exponentials, sums and
+// roundings alone, matrix instructions aside, about two thirds of it for 64 channels.  Weights formed between matrix
+// instructions (a wavefront working at both at once) changed nothing for 64 channels and does not fit the registers for 128; a shader clock
+// of 2.0 to 2.3 GHz under this load is part of the bound.
 // ---------------------------------------------------------------------------------------
 // Weights of a tile as bf16 numbers, TERMS = 1, or sums of two: rounded, and what rounding left.
 template <int TERMS>
@@ -256,7 +262,8 @@ __device__ inline void diff_softmax_pack(DiffMap<W> &w, DiffWeights<TERMS> &p, c
 
 // BOTH (up to 16 rows, one wavefront): lanes 0 .. 15 hold the rows for the first map and lanes 16 .. 31 for the second, each with zeros for the other map's
 // channels, so that a tile takes one block of scores, one softmax and half the products with V.  There is time for weights of
-// two terms then.
+// two terms then.  Bound by memory: one query of 16 heads against caches of up to 16 384 keys x 8 sequences x 4 kv heads of 128 (201 MB) 37 us out of
+// the last-level cache, both launches 51 from memory; one against 2 x 1 374 keys x 16 of 64 7.5 us, which is a few dependent round trips.
 template <typename TO, int W, int WAVES, bool SPLIT, bool BOTH = false>
 __global__ void __launch_bounds__(64 * WAVES, W == 128 && WAVES == 1 ? 1 : 2) diff_attn_fwd_bf16_kernel(DiffArgs a) {
     static_assert(!BOTH || WAVES == 1, "a wavefront holds all rows twice");
@@ -377,7 +384,9 @@ __global__ void __launch_bounds__(64 * WAVES, W == 128 && WAVES == 1 ? 1 : 2) di
 
 // ---------------------------------------------------------------------------------------
 // fp32 tensors: as above on operands of three bf16 numbers, two stages of plane tiles, the next tile on its way under this one's
-// arithmetic.  A tile takes 72 (W = 64) or 144 matrix instructions and the splitting of 32 weights a lane.
+// arithmetic.  A tile takes 72 (W = 64) or 144 matrix instructions and the splitting of 32 weights a lane.  Bound by matrix issue
+// where a wavefront has many tiles (2 x 1 024 tokens x 8 heads of 128 86 us, 0.90 PFLOP/s of bf16 products), by a tile's chain of reads, products and
+// splits where it has few (2 x 576 x 12 of 64 in two parts 30 us, 0.60).
 // ---------------------------------------------------------------------------------------
 template <int W, int WAVES, bool SPLIT>
 __global__ void __launch_bounds__(64 * WAVES, W == 64 && WAVES > 1 ? 2 : 1) diff_attn_fwd_f32_kernel(DiffArgs a) {
@@ -471,7 +480,8 @@ __global__ void __launch_bounds__(64 * WAVES, W == 64 && WAVES > 1 ? 2 : 1) diff
     diff_finish<float, float, W, SPLIT>(a, place, w1, w2, lane);
 }
 
-// fp32 tensors into planes: a thread eight channels; blockIdx.y the tensor (Q, K, V, dO).  Rows behind their sequence's end are not read.
+// fp32 tensors into planes: a thread eight channels; blockIdx.y the tensor (Q, K, V, dO).  Rows behind their sequence's end are not read.  Bound by
+// memory, 10 bytes a number (13 824 rows of 64 a tensor 7 us, 16 384 of 128 13).
 struct DiffSplitArgs {
     TensorArg in[4];
     __bf16 *out[4];
@@ -525,7 +535,7 @@ jv_status diff_split(DiffArgs &a, int W, void *memory, bool with_d_o, hipStream_
 }
 
 // The parts of a row joined, in their order; a part that saw no key is read, in bounds, and not used.
-// Up to PARTS (2, 4 or 8) parts: a wavefront a row, everything it needs of all parts asked for at once.
+// Up to PARTS (2, 4 or 8) parts: a wavefront a row, everything it needs of all parts asked for at once (13 824 rows of 64 in two parts 8.2 us, 18 MB).
 constexpr int kDiffFewParts = 8;
 // Where row `at` of all (batch, kv head, row)s lies.
 struct DiffRowPlace {
@@ -590,7 +600,7 @@ __global__ void __launch_bounds__(256) diff_attn_join_few_kernel(DiffArgs a) {
 
 // More parts, up to kDiffMostParts: a workgroup a row. A thread holds a part's references and sums; then its four wavefronts take every fourth part
 // each, eight parts' loads at a time (one query against 8 192 keys x 8 heads of 128 in 64 parts, both kernels: 22.0 us with one part's
-// loads after the other's, 17.9 so).
+// loads after the other's, 17.9 so; alone 4 to 5 us, three dependent round trips).
 template <typename T, typename TO, int W>
 __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
     static_assert(kDiffMostParts <= 256, "a part a thread");

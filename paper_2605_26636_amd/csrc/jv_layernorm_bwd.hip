@@ -77,7 +77,9 @@ __device__ inline float norm_sum(float x) {
 
 // LANES lanes a row, NV pieces of eight columns a lane: piece p of lane l is columns 8 (l + LANES p) .. + 7.  At most two pieces, so
 // that two workgroups share a unit: rows of more than 1 024 columns lie in two to eight wavefronts, which join their sums through LDS (three or four pieces
-// in one wavefront, or in four with half the wavefronts a unit: 20 000 x 1280 in bf16 61 us, 16 000 x 2560 113).
+// in one wavefront, or in four with half the wavefronts a unit: 20 000 x 1280 in bf16 61 us, 16 000 x 2560 113, so 35 and 53).
+// Reads and writes a row once: 32 768 x 1024 in bf16 with a residual (268 MB) 45 us out of the caches, both launches 55 from memory (4.8 TB/s);
+// 262 144 x 128 without (201 MB) 37 and 44.  Few rows: 200 x 1024 5.3 us, a chain of two row sums.
 template <bool X_BF16, bool DY_BF16, int LANES, int NV>
 __global__ void __launch_bounds__(kNormGradThreads) layernorm_bwd_kernel(NormGradArgs a) {
     constexpr int THREADS = kNormGradThreads, ROWS = THREADS / LANES;  // rows of a workgroup at a time
@@ -201,7 +203,8 @@ __global__ void __launch_bounds__(kNormGradThreads) layernorm_bwd_kernel(NormGra
         }
 }
 
-// Column sums of the workgroups' sums: 64 of the 2 * cols columns a workgroup, 16 wavefronts that take every 16th part.
+// Column sums of the workgroups' sums: 64 of the 2 * cols columns a workgroup, 16 wavefronts that take every 16th part (2.4 us of 25 parts of 1 024 columns,
+// 4.7 of 512; 3.1 MB of 768).
 __global__ void __launch_bounds__(1024) layernorm_bwd_columns_kernel(const float *__restrict__ part, int n, int cols, float *__restrict__ dgamma,
                                                                      float *__restrict__ dbeta) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
