@@ -29,9 +29,10 @@ __global__ void __launch_bounds__(256) diff_attn_rows_kernel(DiffArgs a) {
     const int qi = (int)(row % a.n_q), bh = (int)(row / a.n_q), h = bh % a.heads, b = bh / a.heads;
     float lam = 0.f;
     // (rows of a wavefront may belong to two heads and more)
-    for (int x = __builtin_amdgcn_readfirstlane(bh), last = __builtin_amdgcn_readlane(bh, 63); x <= last; ++x) {
+    const int first = __builtin_amdgcn_readfirstlane(bh), last = __builtin_amdgcn_readlane(bh, 63);
+    for (int x = first; x <= (a.l_step ? last : first); ++x) {
         const float value = diff_lambda<W>(a, x % a.heads, lane).value;
-        if (bh == x) lam = value;
+        if (bh == x || !a.l_step) lam = value;
     }
     float d1 = 0.f, d2 = 0.f;
     if (qi < DiffLengths(a, b).q) {
