@@ -341,6 +341,36 @@ __device__ inline DiffLambda diff_lambda(const DiffArgs &a, int h, int lane) {
     l.value = l.e1 - l.e2 + a.l_init;
     return l;
 }
+// lambda of the lane's head `mine`, one of first .. last, which the wavefront's rows belong to (numbers modulo the heads).  More than two: eight at a
+// time, whose loads and sums go on together (one query of 32 heads against 100 keys of one kv head x 1 024 sequences, a set a head: 53 us one after the
+// other, 44 so).
+template <int W>
+__device__ inline float diff_lambda_of(const DiffArgs &a, int first, int last, int mine, int lane) {
+    if (!a.l_step) return diff_lambda<W>(a, 0, lane).value;
+    float lam = 0.f;
+    if (last - first < 2) {
+        for (int x = first; x <= last; ++x) {
+            const float value = diff_lambda<W>(a, x % a.heads, lane).value;
+            if (mine == x) lam = value;
+        }
+        return lam;
+    }
+    for (int from = first; from <= last; from += 8) {
+        float x1[8], x2[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int at = min(from + u, last) % a.heads * a.l_step + min(lane, W / 2 - 1);
+            x1[u] = a.lq1[at] * a.lk1[at];
+            x2[u] = a.lq2[at] * a.lk2[at];
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const float value = expf(wave_sum(lane < W / 2 ? x1[u] : 0.f)) - expf(wave_sum(lane < W / 2 ? x2[u] : 0.f)) + a.l_init;
+            if (mine == from + u) lam = value;
+        }
+    }
+    return lam;
+}
 
 // Four consecutive channels of an output row.
 __device__ inline void diff_store4(float *p, f32x4 x) { *(f32x4 *)p = x; }

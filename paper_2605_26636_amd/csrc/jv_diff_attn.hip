@@ -151,12 +151,8 @@ __device__ inline void diff_finish(const DiffArgs &a, const DiffPlace &place, co
             }
         return;
     }
-    float lam = 0.f;  // (of the rows' heads one after the other, or the one of all)
-    const int first_head = __builtin_amdgcn_readfirstlane(place.head), last_head = place.kv * a.group + min(place.first + 31, place.n_rows - 1) / a.n_q;
-    for (int h = first_head; h <= (a.l_step ? last_head : first_head); ++h) {
-        const float x = diff_lambda<W>(a, h, lane).value;
-        if (place.head == h || !a.l_step) lam = x;
-    }
+    const int last_head = place.kv * a.group + min(place.first + 31, place.n_rows - 1) / a.n_q;
+    const float lam = diff_lambda_of<W>(a, __builtin_amdgcn_readfirstlane(place.head), last_head, place.head, lane);
     if (!place.row_live) return;
     const float inv1 = l1 > 0.f ? 1.f / l1 : l1, inv2 = l2 > 0.f ? 1.f / l2 : l2;  // (0 for a row that sees nothing, NaN stays NaN)
     const long long row = ((long long)place.b * a.heads + place.head) * a.n_q + place.qi;

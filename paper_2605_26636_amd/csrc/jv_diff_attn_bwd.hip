@@ -27,13 +27,8 @@ __global__ void __launch_bounds__(256) diff_attn_rows_kernel(DiffArgs a) {
     const bool live = at < diff_rows(a);
     const long long row = live ? at : diff_rows(a) - 1;
     const int qi = (int)(row % a.n_q), bh = (int)(row / a.n_q), h = bh % a.heads, b = bh / a.heads;
-    float lam = 0.f;
     // (rows of a wavefront may belong to two heads and more)
-    const int first = __builtin_amdgcn_readfirstlane(bh), last = __builtin_amdgcn_readlane(bh, 63);
-    for (int x = first; x <= (a.l_step ? last : first); ++x) {
-        const float value = diff_lambda<W>(a, x % a.heads, lane).value;
-        if (bh == x || !a.l_step) lam = value;
-    }
+    const float lam = diff_lambda_of<W>(a, __builtin_amdgcn_readfirstlane(bh), __builtin_amdgcn_readlane(bh, 63), bh, lane);
     float d1 = 0.f, d2 = 0.f;
     if (qi < DiffLengths(a, b).q) {
         const u32x4 go = *(const u32x4 *)((const T *)a.d_o.ptr + b * a.d_o.sb + h * a.d_o.sh + qi * a.d_o.sn + ch);

@@ -36,6 +36,69 @@ def test_parts_of_the_gradient(dtype, W, B, H, G, n_q, n_k, causal):
     D.Bounds(x, dtype, causal=causal, backward=True).check(D.run(x, causal=causal, backward=True))
 
 
+@pytest.mark.parametrize("H,G,n_q", [(32, 1, 1), (16, 1, 1), (12, 1, 3), (80, 2, 1), (6, 6, 3)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_a_lambda_a_head_where_a_wavefront_holds_many(dtype, H, G, n_q):
+    x = D.make(H + n_q, 3, H, G, n_q, 40, 64, dtype, per_head=True)
+    out = D.run(x, backward=True)
+    D.Bounds(x, dtype, backward=True).check(out)
+    longer = D.make(H + n_q, 1, H, G, n_q, 700, 64, dtype, per_head=True)
+    D.Bounds(longer, dtype).check(D.run(longer))
+
+
+def test_fp32_output_of_parts():
+    """A bf16 output is an fp32 one, rounded, however the keys are cut."""
+    for H, n_q, n_k in ((2, 8, 70), (2, 8, 140), (2, 8, 330), (2, 8, 2040), (1, 17, 300), (5, 13, 530), (1, 300, 900)):
+        x = D.make(n_k, 1, H, 1, n_q, n_k, 128, "bf16")
+        o32, o16 = (D.run(x, o_dtype=t)["o"] for t in (torch.float32, torch.bfloat16))
+        assert torch.equal(o32.to(torch.bfloat16), o16), (n_q, n_k)
+        D.Bounds(x, "bf16", stored="fp32").check({"o": o32})
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_65535_heads_of_one_key(dtype):
+    """As many (batch, head)s as a call takes.  One key has all weight in both maps: O = (1 - lambda) V, dV = (1 - lambda) dO, dQ = dK = 0,
+    dlambda = -sum dO V.  (1 - lambda) V is formed as V - lambda V, each rounded once; D2 and dP are sums of 64 products."""
+    B, H = 13107, 5
+    x = D.make(26, B, H, H, 1, 1, 64, dtype)
+    out = D.run(x, backward=True)
+    value, e1, e2 = diff.lambdas(tuple(D.host(t) for t in x["lam"]), 0.5, 1)
+    s = 2.0 ** -8 if dtype == "bf16" else D.EPS
+    v, d_o = (D.host(x[n]) for n in ("v", "d_o"))
+    for n, full in (("o", v), ("v", d_o)):
+        D.Bounds.one(n, D.host(out[n]), (1 - value[0]) * full, (s * (1 + 2 * abs(value[0])) + 64 * D.EPS) * abs(full) * 2 + 1e-30)
+    # dS = P (dP - D): the difference of two sums of 64 products, whose rows of O and P2 V are rounded by s; times scale and a row of K or Q
+    size = (abs(d_o) * abs(v)).sum(-1, keepdims=True) * (s * (3 + 2 * abs(value[0])) + 80 * D.EPS) * (1 + abs(value[0])) / 32 ** 0.5
+    for n, other in (("q", "k"), ("k", "q")):
+        D.Bounds.one(n, D.host(out[n]), 0 * v, size * abs(D.host(x[other])) * (1 + 2 * s) + 1e-30)
+    dots = abs(d_o * v).sum()
+    d_value = -(d_o * v).sum()
+    for i, (e, other) in enumerate(((e1, 1), (e1, 0), (-e2, 3), (-e2, 2))):
+        want = d_value * e[0] * D.host(x["lam"][other])
+        D.Bounds.one("lam %d" % i, D.host(out["lam"][i]), want, 100 * D.EPS * (dots + abs(d_value)) * abs(e[0]) * abs(D.host(x["lam"][other])) * 2)
+
+
+def test_a_cache_that_grows_between_replays():
+    """Lengths are read on the GPU: a captured step answers for the caches' present lengths."""
+    x = D.make(27, 3, 8, 2, 1, 1500, 64, "bf16")
+    q, k, v = (x[n].cuda() for n in "qkv")
+    lam = tuple(t.cuda() for t in x["lam"])
+    lengths = torch.zeros(3, dtype=torch.int32, device="cuda")
+    o = torch.empty_like(q)
+    ws = torch.empty(binding.jv_diff_attn_workspace_bytes(binding.make_diff_desc(q, k, v, o, False, None, lengths)), dtype=torch.uint8, device="cuda")
+    binding.jv_diff_attn_fwd(q, k, v, lam, o, lambda_init=0.5, k_lengths=lengths, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        binding.jv_diff_attn_fwd(q, k, v, lam, o, lambda_init=0.5, k_lengths=lengths, workspace=ws)
+    for present in ([0, 1, 2], [1, 33, 700], [1500, 1499, 0], [640, 1500, 31]):
+        lengths.copy_(torch.tensor(present, dtype=torch.int32))
+        o.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        D.Bounds(x, "bf16", lengths=(None, present)).check({"o": o})
+
+
 @pytest.mark.parametrize("dtype,W", [("bf16", 64), ("bf16", 128), ("fp32", 64), ("fp32", 128)])
 def test_lambda_s_gradient_is_not_biased(dtype, W):
     """dlambda_h = -Sum P2 o dP sums numbers of both signs.  Errors of its terms, at most 8 half steps of fp32 each (score, exponential, dP, sum),
