@@ -199,6 +199,8 @@ constexpr bool diff_both_maps(bool bf16, long long n_rows) { return bf16 && n_ro
 // LDS lets; one query token against 16 384 keys x 8 sequences 53 us in 2 048 of them, 41 in 768), at most 256
 // (64 / 256, us: one query against 65 536 keys of 128 x 2 heads 48.3 / 25.6, 32 768 x 4 of 64 21.1 / 17.5, 8 192 fp32 keys x 2 25.2 / 21.7).  Two and four tiles at least, us: one query against 2 x 1 374 keys x 16 heads 11.3 / 12.3, against 300 x 8 11.0 / 14.4, against
 // 4 x 4 096 x 16 19.6 / 18.7 (48 and 32 parts), 40 queries against 2 x 1 024 x 8 14.2 / 12.1, 577 tokens x 8 25.8 / 24.3.
+// Workgroups of four on fp32 rows of 64, two a unit, that fill more than half of the units are cut into three parts of eight tiles at least: 1 374 tokens x
+// 12 heads in one and three 101 / 75, 2 048 x 10 141 / 104, but 2 x 1 024 x 16 in one and two 89 / 97, 7 x 256 x 12 in one and three 36 / 41.
 constexpr int kDiffMostParts = 256;
 struct DiffPlan {
     int waves, blocks, splits, tiles_per_split;
@@ -206,10 +208,11 @@ struct DiffPlan {
 constexpr DiffPlan diff_plan(int B, int kv_heads, long long n_rows, int n_k, int W, bool bf16) {
     const int waves = n_rows <= 64 ? 1 : 4, blocks = (int)((n_rows + 32 * waves - 1) / (32 * waves));
     const long long groups = (long long)B * kv_heads * blocks, tiles = (n_k + kDiffTile - 1) / kDiffTile;
-    const long long holds = waves == 1 ? (bf16 || W == 128 ? 768 : 1536) : bf16 ? 512 : 256;
+    const long long holds = waves == 1 ? (bf16 || W == 128 ? 768 : 1536) : bf16 || W == 64 ? 512 : 256;
     // tiles of a part: four of bf16 tensors (of few rows two, up to 24 parts), one of fp32 ones, whose tiles take 2 us and more
     const long long most = !bf16 ? tiles : diff_both_maps(bf16, n_rows) ? diff_max(tiles / 4, diff_min(tiles / 2, 24)) : tiles / 4;
-    const long long splits = diff_max(1, diff_min(diff_min(groups * 2 > holds ? 1 : holds / groups, most), kDiffMostParts));
+    const bool whole = !bf16 && W == 64 && waves > 1 && groups > 128 ? groups * 3 > holds || tiles < 24 : groups * 2 > holds;
+    const long long splits = diff_max(1, diff_min(diff_min(whole ? 1 : holds / groups, most), kDiffMostParts));
     const int per_split = (int)((tiles + splits - 1) / splits);
     return {waves, blocks, (int)((tiles + per_split - 1) / per_split), per_split};
 }

@@ -46,6 +46,13 @@ def test_a_lambda_a_head_where_a_wavefront_holds_many(dtype, H, G, n_q):
     D.Bounds(longer, dtype).check(D.run(longer))
 
 
+def test_fp32_rows_that_fill_more_than_half_of_the_units():
+    """143 workgroups, and 25 tiles of keys: forward and backward pass are cut."""
+    for W in (64, 128):
+        x = D.make(28, 1, 11, 11, 1537, 800, W, "fp32")
+        D.Bounds(x, "fp32", backward=True).check(D.run(x, backward=True))
+
+
 def test_fp32_output_of_parts():
     """A bf16 output is an fp32 one, rounded, however the keys are cut."""
     for H, n_q, n_k in ((2, 8, 70), (2, 8, 140), (2, 8, 330), (2, 8, 2040), (1, 17, 300), (5, 13, 530), (1, 300, 900)):

@@ -26,7 +26,7 @@ def test_plans_of_the_forward_pass(rule):  # noqa: F811
         assert waves == (1 if rows <= 64 else 4) and 32 * waves * (blocks - 1) < rows <= 32 * waves * blocks
         # no part without a tile, none missing, and no more than a launch or the join takes
         assert 1 <= splits <= 256 and per * splits >= tiles and per * (splits - 1) < tiles
-        holds = 768 if waves == 1 and (bf16 or W == 128) else 1536 if waves == 1 else 512 if bf16 else 256
+        holds = 768 if waves == 1 and (bf16 or W == 128) else 1536 if waves == 1 else 512 if bf16 or W == 64 else 256
         assert splits == 1 or groups * splits <= holds
         assert not bf16 or splits == 1 or per >= (2 if rows <= 16 else 4)
 
