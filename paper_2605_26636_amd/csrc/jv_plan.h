@@ -193,6 +193,22 @@ constexpr long long diff_min(long long x, long long y) { return x < y ? x : y; }
 constexpr long long diff_max(long long x, long long y) { return x > y ? x : y; }
 // Up to 16 rows of bf16 tensors (queries, all heads of a group together) a wavefront holds twice, once for each map.
 constexpr bool diff_both_maps(bool bf16, long long n_rows) { return bf16 && n_rows <= 16; }
+// Parts, up to 16 of two tiles, for workgroups that have a unit each: the fewest tiles one after the other, where a round of 256
+// workgroups costs two more, four where it writes parts, and cutting at all three (a launch that adds the parts).  fp32 tensors, one part / so, us: gradient of keys and values
+// of 1 374 tokens x 12 heads of 64 154 / 117, of 2 304 x 8 248 / 179, of 3 000 x 12 596 / 408; their sum 10 to 18; forward pass of
+// 3 000 x 12 of 128 702 / 556, of 1 374 x 12 171 / 158.
+constexpr int diff_parts_alone(long long items, long long tiles) {
+    long long best = 0;
+    int parts = 1;
+    for (int p = 1; p <= 16 && (p == 1 || 2 * p <= tiles); ++p) {
+        const long long time = (items * p + 255) / 256 * ((tiles + p - 1) / p + (p > 1 ? 4 : 2)) + (p > 1 ? 3 : 0);
+        if (p == 1 || time < best) {
+            best = time;
+            parts = p;
+        }
+    }
+    return parts;
+}
 // How a forward pass is cut: wavefronts a workgroup (32 rows each) and parts of the keys.  Up to 64 rows (a few queries, all heads
 // of a group together) take one wavefront each; more take workgroups of four, which share the tiles.  Keys are cut where
 // the launch would leave units idle: into as many parts as the chip holds workgroups at a time (single wavefronts: three or six a unit, as their
@@ -212,14 +228,16 @@ constexpr DiffPlan diff_plan(int B, int kv_heads, long long n_rows, int n_k, int
     // tiles of a part: four of bf16 tensors (of few rows two, up to 24 parts), one of fp32 ones, whose tiles take 2 us and more
     const long long most = !bf16 ? tiles : diff_both_maps(bf16, n_rows) ? diff_max(tiles / 4, diff_min(tiles / 2, 24)) : tiles / 4;
     const bool whole = !bf16 && W == 64 && waves > 1 && groups > 128 ? groups * 3 > holds || tiles < 24 : groups * 2 > holds;
-    const long long splits = diff_max(1, diff_min(diff_min(whole ? 1 : holds / groups, most), kDiffMostParts));
+    const long long splits = !bf16 && W == 128 && waves > 1 && groups > 16 ? diff_parts_alone(groups, tiles)
+                                                            : diff_max(1, diff_min(diff_min(whole ? 1 : holds / groups, most), kDiffMostParts));
     const int per_split = (int)((tiles + splits - 1) / splits);
     return {waves, blocks, (int)((tiles + per_split - 1) / per_split), per_split};
 }
-// Parts of the tiles that the workgroups of a pass are cut into where they do not fill the chip (512 of bf16 tensors at a time, 256 of fp32
-// ones): as many as fill it, twice that where a causal mask makes some much longer than others; of four tiles at least, of two of fp32
-// tensors, 16 at most.
+// Parts of the tiles that the workgroups of a pass are cut into: of fp32 tensors without a mask as above; else, where they do not fill the chip (512 of
+// bf16 tensors at a time, 256 of fp32 ones), as many as fill it, twice that where a causal mask makes some much longer than others; of four tiles at
+// least, of two of fp32 tensors, 16 at most.
 constexpr int diff_bwd_parts(long long items, long long tiles, bool bf16, bool causal) {
+    if (!bf16 && !causal) return diff_parts_alone(items, tiles);
     const long long holds = (bf16 ? 512 : 256) * (causal ? 2 : 1);
     return (int)diff_max(1, diff_min(diff_min(holds / items, tiles / (bf16 ? 4 : 2)), 16));
 }

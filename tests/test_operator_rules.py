@@ -27,7 +27,8 @@ def test_plans_of_the_forward_pass(rule):  # noqa: F811
         # no part without a tile, none missing, and no more than a launch or the join takes
         assert 1 <= splits <= 256 and per * splits >= tiles and per * (splits - 1) < tiles
         holds = 768 if waves == 1 and (bf16 or W == 128) else 1536 if waves == 1 else 512 if bf16 or W == 64 else 256
-        assert splits == 1 or groups * splits <= holds
+        alone = not bf16 and W == 128 and waves > 1 and groups > 16   # see test_parts_of_workgroups_with_a_unit_each
+        assert splits == 1 or (splits <= 16 if alone else groups * splits <= holds)
         assert not bf16 or splits == 1 or per >= (2 if rows <= 16 else 4)
 
 
@@ -50,7 +51,8 @@ def test_parts_of_the_gradient(rule):  # noqa: F811
     got = rule([f"diff_bwd_parts({i}ll, {t}ll, {b}, {c})" for i, t, b, c in cases])
     for (items, tiles, bf16, causal), parts in zip(cases, got):
         assert 1 <= parts <= 16 and parts <= max(1, tiles // (4 if bf16 else 2))
-        assert parts == 1 or items * parts <= (512 if bf16 else 256) * (2 if causal else 1)
+        if bf16 or causal:
+            assert parts == 1 or items * parts <= (512 if bf16 else 256) * (2 if causal else 1)
     for bf16 in (0, 1):   # what the GPU tests reach: one part, several, and the most, of either pass
         q, k = set(), set()
         for B, H, G, n_q, n_k, causal in V.GRADIENTS:
@@ -61,6 +63,14 @@ def test_parts_of_the_gradient(rule):  # noqa: F811
             k.add(p[1])
         for parts in (q, k):
             assert 1 in parts and 16 in parts and parts & set(range(2, 16)), (bf16, q, k)
+
+
+def test_parts_of_workgroups_with_a_unit_each(rule):  # noqa: F811
+    """No number of parts up to 16 of two tiles takes fewer tiles one after the other, by the rule's count of them."""
+    cases = [(items, tiles) for items in (1, 17, 100, 128, 129, 132, 256, 257, 288, 511, 5000, 1 << 30) for tiles in (1, 2, 3, 8, 18, 43, 94, 1 << 19)]
+    for (items, tiles), got in zip(cases, rule([f"diff_parts_alone({i}ll, {t}ll)" for i, t in cases])):
+        time = {p: -(-items * p // 256) * (-(-tiles // p) + (4 if p > 1 else 2)) + (3 if p > 1 else 0) for p in range(1, 17) if p == 1 or 2 * p <= tiles}
+        assert time[got] == min(time.values()) and got == min(p for p in time if time[p] == time[got])
 
 
 def test_rows_and_workgroups_of_a_norm(rule):  # noqa: F811
