@@ -180,20 +180,20 @@ struct DiffQueries {
     }
 };
 
-// Scores and dP of a tile (rows: keys) become the gradients of the logits, in place.
-// For lambda, bf16 tensors add up e2 dP here: their D2 holds the rounding of P2 V's weights and rows, which shows in a sum of so many signs.  fp32
-// tensors add up D2 (diff_attn_dq_f32_kernel).
-template <bool LAMBDA>
-__device__ inline void diff_logit_grads(f32x16 &s1, f32x16 &s2, const f32x16 &dp, const DiffRowGrad &r, float c, float &lam_sum) {
+// Scores and dP of a tile (rows: keys) become the gradients of the logits, in place; returns the lane's sum of e2 dP.
+// For lambda, bf16 tensors add these up, tile by tile (one sum over 2 048 products was off four times as far): their D2 holds the rounding of P2 V's
+// weights and rows, which shows in a sum of so many signs.  fp32 tensors add up D2 (diff_attn_dq_f32_kernel).
+__device__ inline float diff_logit_grads(f32x16 &s1, f32x16 &s2, const f32x16 &dp, const DiffRowGrad &r, float c) {
+    float sum = 0.f;
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
         const float e1 = __builtin_amdgcn_exp2f(fmaf(s1[v], c, r.minus_m1)), e2 = __builtin_amdgcn_exp2f(fmaf(s2[v], c, r.minus_m2));
-        if (LAMBDA) lam_sum = fmaf(e2, dp[v], lam_sum);
+        sum = fmaf(e2, dp[v], sum);
         s1[v] = e1 * fmaf(dp[v], r.f1, r.h1);
         s2[v] = e2 * fmaf(dp[v], r.f2, r.h2);
     }
+    return sum;
 }
-
 // dQ, and the sums of P2 o dP (for lambda): a wavefront keeps 32 queries of one head, their dO and their dQ, and walks the keys.
 // A tile takes W / 16 score products, as many of V with dO, and as many of K^T with the gradients of the logits.  Tiles come straight
 // into two LDS stages, the next tile's under this one's arithmetic.  Bound by the issue of matrix and vector instructions: 4 x 4 096 tokens x 8 heads of
@@ -231,6 +231,15 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dq_bf16_kernel(DiffArgs a) {
             go[ks] = diff_global_frag(grow, ks, g, p.limit > 0);
         }
         r.load(a, p.row, p.limit > 0, lam);
+    }
+    // Every other query works with -dO and -dP: the matrix unit's sums lie a little low (2e-10 of their terms), whatever their sign, which the sums for
+    // lambda would add up over all queries and heads.
+    if (lane & 1) {
+#pragma unroll
+        for (int ks = 0; ks < 2 * KS; ++ks) go[ks] = as_bf16x8(as_u32x4(go[ks]) ^ 0x80008000u);
+        r.f1 = -r.f1;
+        r.f2 = -r.f2;
+        r.inv2 = -r.inv2;
     }
 #pragma unroll
     for (int ks = 0; ks < 2 * KS; ++ks) asm volatile("" : "+v"(q[ks]), "+v"(go[ks]));  // (waited for here, not inside the loop)
@@ -273,7 +282,7 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dq_bf16_kernel(DiffArgs a) {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) dp = mfma32(as_bf16x8(y[ks]), go[KS + ks], dp);
         if ((tile + 1) * kDiffTile > p.least) diff_hide_keys(s1, s2, tile * kDiffTile, p.limit > 0 ? p.limit : a.n_k + kDiffTile, g);
-        diff_logit_grads<true>(s1, s2, dp, r, a.c, lam_sum);
+        lam_sum += diff_logit_grads(s1, s2, dp, r, a.c);
         bf16x8 ds1[2], ds2[2];
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
@@ -368,8 +377,7 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dq_f32_kernel(DiffArgs a) {
         diff_read_cols3<W, 0, 0>(v[0], cols, 0);
         __builtin_amdgcn_sched_barrier(0);
         if ((tile + 1) * kDiffTile > p.least) diff_hide_keys(s1, s2, tile * kDiffTile, p.limit > 0 ? p.limit : a.n_k + kDiffTile, g);
-        float none = 0.f;
-        diff_logit_grads<false>(s1, s2, dp, r, a.c, none);
+        diff_logit_grads(s1, s2, dp, r, a.c);
         diff_landed(v[0]);
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
