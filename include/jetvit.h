@@ -281,7 +281,7 @@ jv_status jv_full_attn_fwd(const jv_attn_desc *desc, const void *q, const void *
  *  - causal != 0: query i sees keys 0 .. i + k_lengths[b] - q_lengths[b] (the last query sees all keys).
  *  - A query that sees no key has a zero row in O and in dQ.
  * head_dim is 64 or 128 for both element types, o_dtype as in jv_attn_desc; at most 2^24 queries and keys, 2^30 queries of the
- * heads that share K and V, and 65535 batch entries times heads.  Strides as in jv_attn_desc, stride_n up to 2^25; K and V may
+ * heads that share K and V, 65535 batch entries times heads, and 2^32 - 2^16 queries, and keys, of all heads together.  Strides as in jv_attn_desc, stride_n up to 2^25; K and V may
  * be broadcast (stride 0), rows of O may not overlap each other.  The stride of an axis of one is ignored.
  * scale <= 0 or NaN selects 1/sqrt(d); one of its own lies between 1e-30 and 1e30.
  * Arithmetic: JV_F32 as sums of three bf16 numbers (see the conventions above); an infinity among the operands gives NaN.

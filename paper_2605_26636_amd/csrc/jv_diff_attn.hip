@@ -103,14 +103,18 @@ struct DiffPlace {
         split = item.part;
         bkv = item.bh;
         // (causal: the last blocks of all heads of a group before the ones before them)
-        const int per_head = a.blocks / a.group, block = a.causal && per_head * a.group == a.blocks ? item.block % a.group * per_head + item.block / a.group : item.block;
-        b = bkv / a.kv_heads;
-        kv = bkv % a.kv_heads;
+        int block = item.block;
+        if (a.causal) {
+            const unsigned group = a.group, per_head = (unsigned)a.blocks / group;
+            if (per_head * group == (unsigned)a.blocks) block = (unsigned)block % group * per_head + (unsigned)block / group;
+        }
+        b = (unsigned)bkv / (unsigned)a.kv_heads;
+        kv = bkv - b * a.kv_heads;
         n_rows = a.group * a.n_q;
         first = (block * WAVES + wave) * 32;
         r = first + li;
         row_live = r < n_rows;
-        const int hg = row_live ? r / a.n_q : 0;
+        const int hg = row_live ? (unsigned)r / (unsigned)a.n_q : 0;
         qi = row_live ? r - hg * a.n_q : 0;
         head = kv * a.group + hg;
         return true;
@@ -491,7 +495,8 @@ __global__ void __launch_bounds__(256) diff_attn_split_kernel(DiffSplitArgs a) {
     const int t = blockIdx.y;
     const long long at = (long long)blockIdx.x * 256 + threadIdx.x, row = at / (W / 8);
     if (row >= a.rows[t]) return;
-    const int ch = (int)(at % (W / 8)) * 8, i = (int)(row % a.n[t]), bh = (int)(row / a.n[t]), h = bh % a.heads[t], b = bh / a.heads[t];
+    const unsigned bh = (unsigned)row / (unsigned)a.n[t], b = bh / (unsigned)a.heads[t];
+    const int ch = (int)(at % (W / 8)) * 8, i = (int)((unsigned)row - bh * a.n[t]), h = (int)(bh - b * a.heads[t]);
     if (a.len[t] && i >= a.len[t][b]) return;
     const TensorArg &in = a.in[t];
     const float *from = (const float *)in.ptr + b * in.sb + h * in.sh + i * in.sn + ch;
@@ -538,11 +543,11 @@ constexpr int kDiffFewParts = 8;
 struct DiffRowPlace {
     int b, head, qi;
     long long row;
-    __device__ DiffRowPlace(const DiffArgs &a, long long at) {
-        const int n_rows = a.group * a.n_q, bkv = (int)(at / n_rows), r = (int)(at % n_rows), hg = r / a.n_q;
-        b = bkv / a.kv_heads;
+    __device__ DiffRowPlace(const DiffArgs &a, unsigned at) {
+        const unsigned n_rows = a.group * a.n_q, bkv = at / n_rows, r = at - bkv * n_rows, hg = r / (unsigned)a.n_q;
+        b = bkv / (unsigned)a.kv_heads;
         qi = r - hg * a.n_q;
-        head = bkv % a.kv_heads * a.group + hg;
+        head = (bkv - b * a.kv_heads) * a.group + hg;
         row = ((long long)b * a.heads + head) * a.n_q + qi;
     }
 };
@@ -552,7 +557,7 @@ __global__ void __launch_bounds__(256) diff_attn_join_few_kernel(DiffArgs a) {
     const int lane = threadIdx.x & 63;
     const long long all = diff_rows(a), at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (at >= all) return;
-    const DiffRowPlace place(a, at);
+    const DiffRowPlace place(a, (unsigned)at);
     f32x4 ml[PARTS];
     float x1[PARTS][PER], x2[PARTS][PER];
 #pragma unroll
@@ -604,7 +609,7 @@ __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const long long all = diff_rows(a), at = blockIdx.x;
     __shared__ float sums[4][2 * W], top[2][4], total[2][4], factor[2][256];
-    const DiffRowPlace place(a, at);
+    const DiffRowPlace place(a, (unsigned)at);
     f32x4 ml = {-INFINITY, 0.f, -INFINITY, 0.f};
     if ((int)threadIdx.x < a.splits) ml = *(const f32x4 *)(a.part + ((long long)threadIdx.x * all + at) * (2 * W + 4));
     float m1 = ml[0], m2 = ml[2];
@@ -710,6 +715,8 @@ jv_status diff_check_desc(const jv_diff_attn_desc *d) {
     if (d->heads % d->kv_heads) return fail(JV_ERR_INVALID_ARG, "heads must be a multiple of kv_heads");
     if (d->n_q > (1 << 24) || d->n_k > (1 << 24)) return fail(JV_ERR_UNSUPPORTED, "more than 2^24 queries or keys");
     if ((int64_t)d->batch * d->heads > 65535) return fail(JV_ERR_UNSUPPORTED, "batch * heads above 65535");
+    if ((int64_t)d->batch * d->heads * d->n_q > 0xffff0000ll || (int64_t)d->batch * d->kv_heads * d->n_k > 0xffff0000ll)
+        return fail(JV_ERR_UNSUPPORTED, "more than 2^32 - 2^16 rows of queries or keys");
     if ((int64_t)d->heads / d->kv_heads * d->n_q > (1 << 30)) return fail(JV_ERR_UNSUPPORTED, "more than 2^30 queries of a kv head");
     if (d->head_dim <= 0) return fail(JV_ERR_INVALID_ARG, "head_dim must be positive");
     if (d->head_dim != kHeadDim && d->head_dim != kHeadDimWide) return fail(JV_ERR_UNSUPPORTED, "head_dim must be 64 or 128");

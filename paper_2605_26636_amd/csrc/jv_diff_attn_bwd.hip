@@ -26,7 +26,7 @@ __global__ void __launch_bounds__(256) diff_attn_rows_kernel(DiffArgs a) {
     const int ch = (threadIdx.x % LANES) * PER;
     const bool live = at < diff_rows(a);
     const long long row = live ? at : diff_rows(a) - 1;
-    const int qi = (int)(row % a.n_q), bh = (int)(row / a.n_q), h = bh % a.heads, b = bh / a.heads;
+    const int bh = (int)((unsigned)row / (unsigned)a.n_q), qi = (int)((unsigned)row - (unsigned)bh * a.n_q), b = (unsigned)bh / (unsigned)a.heads, h = bh - b * a.heads;
     // (rows of a wavefront may belong to two heads and more)
     const float lam = diff_lambda_of<W>(a, __builtin_amdgcn_readfirstlane(bh), __builtin_amdgcn_readlane(bh, 63), bh, lane);
     float d1 = 0.f, d2 = 0.f;
@@ -80,8 +80,8 @@ __global__ void __launch_bounds__(256) diff_attn_rows_kernel(DiffArgs a) {
 
 // One of a.parts equal parts of `total`: [from, to).
 __device__ inline void diff_part(const DiffArgs &a, int part, int total, int *from, int *to) {
-    *from = (int)((long long)total * part / a.parts);
-    *to = (int)((long long)total * (part + 1) / a.parts);
+    *from = (unsigned)total * part / (unsigned)a.parts;  // (at most 2^25 tiles and a head's share of one each, 16 parts)
+    *to = (unsigned)total * (part + 1) / (unsigned)a.parts;
 }
 
 // What the query pass knows of a query: its weights are e inv with e = 2^(c score - m), and the gradients of its logits
@@ -156,9 +156,9 @@ struct DiffQueries {
         part = item.part;
         block = item.block;
         const int bh = item.bh;
-        b = bh / a.heads;
-        h = bh % a.heads;
-        kv = h / a.group;
+        b = (unsigned)bh / (unsigned)a.heads;
+        h = bh - b * a.heads;
+        kv = (unsigned)h / (unsigned)a.group;
         qi = (block * 4 + wave) * 32 + (lane & 31);
         row_live = qi < a.n_q;
         row = (long long)bh * a.n_q + qi;
@@ -410,8 +410,8 @@ struct DiffKeys {
         part = item.part;
         block = item.block;
         const int bkv = item.bh;
-        b = bkv / a.kv_heads;
-        kv = bkv % a.kv_heads;
+        b = (unsigned)bkv / (unsigned)a.kv_heads;
+        kv = bkv - b * a.kv_heads;
         const DiffLengths len(a, b);
         len_q = len.q;
         len_k = len.k;
@@ -851,17 +851,17 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
 // from W on to `out2`.  Rows behind a sequence's end hold zeros in every part.  Bound by memory (32 768 rows of dK and dV of 128 in four parts, 134 MB, 26 us).
 template <typename T, int W>
 __global__ void __launch_bounds__(256) diff_attn_sum_kernel(const float *part, int parts, long long rows, int heads, int n, TensorArg out, TensorArg out2, int channels) {
-    const int per_row = channels / 4;
-    const long long at = (long long)blockIdx.x * 256 + threadIdx.x, row = at / per_row;
+    const unsigned per_row = channels / 4;  // (divides 256)
+    const long long row = (long long)blockIdx.x * (256 / per_row) + threadIdx.x / per_row;
     if (row >= rows) return;
-    const int ch = (int)(at % per_row) * 4;
+    const int ch = (int)(threadIdx.x % per_row) * 4;
     f32x4 sum = *(const f32x4 *)(part + row * channels + ch);
     for (int p = 1; p < parts; ++p) {
         const f32x4 x = *(const f32x4 *)(part + (p * rows + row) * channels + ch);
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] += x[e];
     }
-    const int i = (int)(row % n), bh = (int)(row / n), h = bh % heads, b = bh / heads;
+    const int bh = (int)((unsigned)row / (unsigned)n), i = (int)((unsigned)row - (unsigned)bh * n), b = (unsigned)bh / (unsigned)heads, h = bh - b * heads;
     const TensorArg &to = ch < W ? out : out2;
     diff_store4((T *)const_cast<void *>(to.ptr) + b * to.sb + h * to.sh + i * to.sn + (ch < W ? ch : ch - W), sum);
 }
@@ -879,7 +879,10 @@ __global__ void __launch_bounds__(1024) diff_attn_dlambda_kernel(DiffArgs a) {
         double sum = 0.0;
         if (a.l_step) {
             const long long n = (long long)a.B * sums;
-            for (long long x = lane; x < n; x += 64) sum += a.lam_part[x / sums * per_image + (long long)set * sums + x % sums];
+            for (long long x = lane; x < n; x += 64) {
+                const unsigned image = (unsigned)x / (unsigned)sums;
+                sum += a.lam_part[image * per_image + (long long)set * sums + ((unsigned)x - image * sums)];
+            }
         } else {
             for (long long x = threadIdx.x; x < a.B * per_image; x += blockDim.x) sum += a.lam_part[x];
         }

@@ -62,6 +62,15 @@ def test_descriptors_that_are_refused(field, value, status):
     assert forward(d) == status and backward(d) == status and queries(d) == [0, 0, 0]
 
 
+def test_more_rows_than_32_bits_count():
+    """Queries, or keys, of all heads together (heads that share one row through a stride of zero count each)."""
+    for change in (dict(B=16384, H=4, G=4, n_q=1 << 16, n_k=8), dict(B=16384, H=4, G=4, n_q=8, n_k=1 << 16)):
+        d = desc(**change)
+        for s in (d.q, d.k, d.v):
+            s.stride_b = s.stride_h = 0
+        assert forward(d) == UNSUPPORTED and backward(d) == UNSUPPORTED and binding.jv_diff_attn_workspace_bytes(d) == 0
+
+
 def test_strides_that_are_refused():
     for name in "qkvo":
         for field, value in (("stride_n", 32), ("stride_n", 66), ("stride_h", -64), ("stride_b", 1 << 62)):
