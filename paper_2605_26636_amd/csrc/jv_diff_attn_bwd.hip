@@ -847,30 +847,38 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
     diff_finish_dkv<float, W>(a, dk, dv, p, g);
 }
 
-// Parts of rows of `channels` fp32 numbers added in their order: row (x, h, n) of B x heads x n rows to tensor `out`, and its channels
-// from W on to `out2`.  Rows behind a sequence's end hold zeros in every part.  Bound by memory (32 768 rows of dK and dV of 128 in four parts, 134 MB, 26 us).
+// Parts of rows of `channels` fp32 numbers to be added in their order: row (x, h, n) of B x heads x n rows goes to tensor `out`, and its channels
+// from W on to `out2`.  Rows behind a sequence's end hold zeros in every part.
+constexpr int kDiffFinishThreads = 1024;
+struct DiffSum {
+    const float *part;
+    int parts, heads, n, channels;
+    long long rows;
+    TensorArg out, out2;
+    unsigned blocks;  // workgroups, 0 without parts
+};
 template <typename T, int W>
-__global__ void __launch_bounds__(256) diff_attn_sum_kernel(const float *part, int parts, long long rows, int heads, int n, TensorArg out, TensorArg out2, int channels) {
-    const unsigned per_row = channels / 4;  // (divides 256)
-    const long long row = (long long)blockIdx.x * (256 / per_row) + threadIdx.x / per_row;
-    if (row >= rows) return;
+__device__ inline void diff_add_parts(const DiffSum &a, unsigned block) {
+    const unsigned per_row = a.channels / 4;  // (divides the threads)
+    const long long row = (long long)block * (kDiffFinishThreads / per_row) + threadIdx.x / per_row;
+    if (row >= a.rows) return;
     const int ch = (int)(threadIdx.x % per_row) * 4;
-    f32x4 sum = *(const f32x4 *)(part + row * channels + ch);
-    for (int p = 1; p < parts; ++p) {
-        const f32x4 x = *(const f32x4 *)(part + (p * rows + row) * channels + ch);
+    f32x4 sum = *(const f32x4 *)(a.part + row * a.channels + ch);
+    for (int p = 1; p < a.parts; ++p) {
+        const f32x4 x = *(const f32x4 *)(a.part + (p * a.rows + row) * a.channels + ch);
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] += x[e];
     }
-    const int bh = (int)((unsigned)row / (unsigned)n), i = (int)((unsigned)row - (unsigned)bh * n), b = (unsigned)bh / (unsigned)heads, h = bh - b * heads;
-    const TensorArg &to = ch < W ? out : out2;
+    const int bh = (int)((unsigned)row / (unsigned)a.n), i = (int)((unsigned)row - (unsigned)bh * a.n), b = (unsigned)bh / (unsigned)a.heads, h = bh - b * a.heads;
+    const TensorArg &to = ch < W ? a.out : a.out2;
     diff_store4((T *)const_cast<void *>(to.ptr) + b * to.sb + h * to.sh + i * to.sn + (ch < W ? ch : ch - W), sum);
 }
 
 // Gradients of lambda's vectors from the sums of P2 o dP: dlambda_h is their negative sum, over the heads too where these share
-// the vectors.  One workgroup of as many wavefronts as there are sets, 16 at most; sums in 64 bits.  4 to 5 us, a launch and a few round trips.
+// the vectors.  One workgroup, a wavefront a set; sums in 64 bits.
 template <int W>
-__global__ void __launch_bounds__(1024) diff_attn_dlambda_kernel(DiffArgs a) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+__device__ inline void diff_lambda_grads(const DiffArgs &a) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = kDiffFinishThreads / 64;
     __shared__ double shared_sum[16];
     const int sets = a.l_step ? a.heads : 1;
     const int sums = a.blocks * a.parts;  // of a (batch, head)
@@ -884,7 +892,7 @@ __global__ void __launch_bounds__(1024) diff_attn_dlambda_kernel(DiffArgs a) {
                 sum += a.lam_part[image * per_image + (long long)set * sums + ((unsigned)x - image * sums)];
             }
         } else {
-            for (long long x = threadIdx.x; x < a.B * per_image; x += blockDim.x) sum += a.lam_part[x];
+            for (long long x = threadIdx.x; x < a.B * per_image; x += kDiffFinishThreads) sum += a.lam_part[x];
         }
 #pragma unroll
         for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
@@ -906,6 +914,16 @@ __global__ void __launch_bounds__(1024) diff_attn_dlambda_kernel(DiffArgs a) {
             a.dlk2[at] = -dl * l.e2 * q2;
         }
     }
+}
+
+// What is left behind both passes, in one launch: parts of dK and dV, parts of dQ, and lambda's gradients.  Three launches were 5 us each for small calls; the
+// parts are bound by memory (32 768 rows of dK and dV of 128 in four parts, 134 MB, 26 us).
+template <typename T, int W>
+__global__ void __launch_bounds__(kDiffFinishThreads) diff_attn_finish_kernel(DiffArgs a, DiffSum keys, DiffSum queries) {
+    const unsigned block = blockIdx.x;
+    if (block < keys.blocks) diff_add_parts<T, W>(keys, block);
+    else if (block < keys.blocks + queries.blocks) diff_add_parts<T, W>(queries, block - keys.blocks);
+    else diff_lambda_grads<W>(a);
 }
 
 struct DiffBwdPlan {
@@ -943,26 +961,19 @@ static jv_status diff_backward(DiffArgs a, const DiffBwdPlan &plan, void *planes
     if constexpr (BF16) hipLaunchKernelGGL((diff_attn_dkv_bf16_kernel<W>), dim3(diff_grid(a.items)), dim3(256), 0, stream, a);
     else hipLaunchKernelGGL((diff_attn_dkv_f32_kernel<W>), dim3(diff_grid(a.items)), dim3(256), 0, stream, a);
     if ((st = launch_status("diff_attn_dkv_kernel")) != JV_OK) return st;
-    if (a.parts > 1) {
-        hipLaunchKernelGGL((diff_attn_sum_kernel<T, W>), dim3((unsigned)((keys * (W / 2) + 255) / 256)), dim3(256), 0, stream, (const float *)a.dkv_part, a.parts, keys,
-                           a.kv_heads, a.n_k, a.dk, a.dv, 2 * W);
-        if ((st = launch_status("diff_attn_sum_kernel")) != JV_OK) return st;
-    }
     a.blocks = plan.q_blocks;
     a.parts = plan.q_parts;
     a.items = (long long)a.B * a.heads * a.blocks * a.parts;
     if constexpr (BF16) hipLaunchKernelGGL((diff_attn_dq_bf16_kernel<W>), dim3(diff_grid(a.items)), dim3(256), 0, stream, a);
     else hipLaunchKernelGGL((diff_attn_dq_f32_kernel<W>), dim3(diff_grid(a.items)), dim3(256), 0, stream, a);
     if ((st = launch_status("diff_attn_dq_kernel")) != JV_OK) return st;
-    if (a.parts > 1) {
-        hipLaunchKernelGGL((diff_attn_sum_kernel<T, W>), dim3((unsigned)((rows * (W / 4) + 255) / 256)), dim3(256), 0, stream, (const float *)a.dq_part, a.parts, rows, a.heads,
-                           a.n_q, a.dq, a.dq, W);
-        if ((st = launch_status("diff_attn_sum_kernel")) != JV_OK) return st;
-    }
-    if (!a.dlq1) return JV_OK;
-    const int waves = a.l_step ? (a.heads < 16 ? a.heads : 16) : 16;
-    hipLaunchKernelGGL((diff_attn_dlambda_kernel<W>), dim3(1), dim3(64 * waves), 0, stream, a);
-    return launch_status("diff_attn_dlambda_kernel");
+    auto blocks = [](int parts, long long n, int channels) { return parts > 1 ? (unsigned)((n * (channels / 4) + kDiffFinishThreads - 1) / kDiffFinishThreads) : 0u; };
+    const DiffSum k{a.dkv_part, plan.k_parts, a.kv_heads, a.n_k, 2 * W, keys, a.dk, a.dv, blocks(plan.k_parts, keys, 2 * W)};
+    const DiffSum q{a.dq_part, plan.q_parts, a.heads, a.n_q, W, rows, a.dq, a.dq, blocks(plan.q_parts, rows, W)};
+    const unsigned grid = k.blocks + q.blocks + (a.dlq1 ? 1 : 0);
+    if (!grid) return JV_OK;
+    hipLaunchKernelGGL((diff_attn_finish_kernel<T, W>), dim3(grid), dim3(kDiffFinishThreads), 0, stream, a, k, q);
+    return launch_status("diff_attn_finish_kernel");
 }
 
 }  // namespace jv
