@@ -285,6 +285,10 @@ jv_status jv_full_attn_fwd(const jv_attn_desc *desc, const void *q, const void *
  * be broadcast (stride 0), rows of O may not overlap each other.  The stride of an axis of one is ignored.
  * scale <= 0 or NaN selects 1/sqrt(d); one of its own lies between 1e-30 and 1e30.
  * Arithmetic: JV_F32 as sums of three bf16 numbers (see the conventions above); an infinity among the operands gives NaN.
+ * A logit of -inf (of finite numbers whose product overflows, too) weighs nothing in its map and leaves the other map alone; a map whose
+ * logits are all -inf weighs nothing, as one that sees no key; a logit of +inf and NaN in a query are NaN in its row of O and what
+ * follows from it, however the keys are cut.  A key or value that is not finite and that causal queries see may reach others of its sequence,
+ * which meet it with a weight of 0.
  * JV_BF16: the weights Pm are rounded to bf16 in front of the product with V (up to 16 queries of the heads that share K and V: to
  * the sum of two bf16 numbers), and in the gradient P1 - lambda P2 and the gradients of the logits in front of theirs; everything
  * else is fp32.

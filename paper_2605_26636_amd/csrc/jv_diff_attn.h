@@ -25,7 +25,7 @@ struct DiffArgs {
     const float *lq1, *lk1, *lq2, *lk2;
     float l_init;
     int l_step;                     // W / 2: a set of vectors for every head; 0: one set
-    float *ml;                      // saved: [4][B * heads * n_q], reference m of the first map (log2 units; +inf: sees no key), sum l of
+    float *ml;                      // saved: [4][B * heads * n_q], reference m of the first map (log2 units; +inf: no weight), sum l of
                                     // exp2(logit - m), then those of the second; or null
     void *o2;                       // saved: [B * heads * n_q][W], P2 V
     // forward pass over parts of the keys

@@ -121,12 +121,17 @@ struct DiffPlace {
     }
 };
 
-// What the backward pass needs of a row: both references and sums.
+// What the backward pass needs of a row: both references and sums.  A map without a weight (no key seen, or logits of -inf alone) has m = +inf; a
+// reference of +inf, and that of a row of NaN, which m does not show, are NaN.
+__device__ inline float diff_saved_reference(float m, float l) {
+    if (m == -INFINITY && l == 0.f) return INFINITY;
+    return fabsf(m) == INFINITY ? NAN : m;
+}
 __device__ inline void diff_save(const DiffArgs &a, long long row, float m1, float l1, float m2, float l2) {
     const long long n = diff_rows(a);
-    a.ml[row] = m1 == -INFINITY ? INFINITY : m1;
+    a.ml[row] = diff_saved_reference(m1, l1);
     a.ml[n + row] = l1;
-    a.ml[2 * n + row] = m2 == -INFINITY ? INFINITY : m2;
+    a.ml[2 * n + row] = diff_saved_reference(m2, l2);
     a.ml[3 * n + row] = l2;
 }
 
@@ -144,7 +149,7 @@ __device__ inline void diff_finish(const DiffArgs &a, const DiffPlace &place, co
         if (!place.row_live) return;
         float *part = a.part + ((long long)place.split * a.B * a.kv_heads * place.n_rows + (long long)place.bkv * place.n_rows + place.r) * (2 * W + 4);
         if (g == 0) *(f32x4 *)part = f32x4{w1.m, l1, w2.m, l2};
-        if (w1.m == -INFINITY && w2.m == -INFINITY) return;  // no key of this part is seen: not read again either
+        if (w1.m == -INFINITY && w2.m == -INFINITY) return;  // no key of this part is seen, or all logits are -inf or NaN: not read again either
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
@@ -158,7 +163,7 @@ __device__ inline void diff_finish(const DiffArgs &a, const DiffPlace &place, co
     const int last_head = place.kv * a.group + min(place.first + 31, place.n_rows - 1) / a.n_q;
     const float lam = diff_lambda_of<W>(a, __builtin_amdgcn_readfirstlane(place.head), last_head, place.head, lane);
     if (!place.row_live) return;
-    const float inv1 = l1 > 0.f ? 1.f / l1 : l1, inv2 = l2 > 0.f ? 1.f / l2 : l2;  // (0 for a row that sees nothing, NaN stays NaN)
+    const float inv1 = l1 > 0.f ? 1.f / l1 : l1, inv2 = l2 > 0.f ? 1.f / l2 : l2;  // (0 for a map without a weight, NaN stays NaN)
     const long long row = ((long long)place.b * a.heads + place.head) * a.n_q + place.qi;
     if (a.ml && g == 0) diff_save(a, row, w1.m, l1, w2.m, l2);
     TO *o = (TO *)const_cast<void *>(a.o.ptr) + place.b * a.o.sb + place.head * a.o.sh + place.qi * a.o.sn;
@@ -536,7 +541,10 @@ jv_status diff_split(DiffArgs &a, int W, void *memory, bool with_d_o, hipStream_
     return launch_status("diff_attn_split_kernel");
 }
 
-// The parts of a row joined, in their order; a part that saw no key is read, in bounds, and not used.
+// The parts of a row joined, in their order.  Each map asks for its own reference: a part may have weights in one of them alone (logits of -inf in the
+// other), and one of -inf has a sum of 0, or of NaN, which m does not show and the total must.  Unnormalised outputs of a part where both
+// references are -inf were not written: read, in bounds, and not used.
+__device__ inline float diff_join_factor(float m, float top) { return m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top); }
 // Up to PARTS (2, 4 or 8) parts: a wavefront a row, everything it needs of all parts asked for at once (13 824 rows of 64 in two parts 8.2 us, 18 MB).
 constexpr int kDiffFewParts = 8;
 // Where row `at` of all (batch, kv head, row)s lies.
@@ -579,10 +587,11 @@ __global__ void __launch_bounds__(256) diff_attn_join_few_kernel(DiffArgs a) {
     }
 #pragma unroll
     for (int s = 0; s < PARTS; ++s) {
-        if (s >= a.splits || ml[s][0] == -INFINITY) continue;  // (uniform; both maps see the same keys)
-        const float f1 = __builtin_amdgcn_exp2f(ml[s][0] - m1), f2 = __builtin_amdgcn_exp2f(ml[s][2] - m2);
+        if (s >= a.splits) continue;  // (uniform)
+        const float f1 = diff_join_factor(ml[s][0], m1), f2 = diff_join_factor(ml[s][2], m2);
         l1 = fmaf(ml[s][1], f1, l1);
         l2 = fmaf(ml[s][3], f2, l2);
+        if (ml[s][0] == -INFINITY && ml[s][2] == -INFINITY) continue;  // (uniform)
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
             y1[e] = fmaf(x1[s][e], f1, y1[e]);
@@ -625,11 +634,11 @@ __global__ void __launch_bounds__(256) diff_attn_join_kernel(DiffArgs a) {
     __syncthreads();
     m1 = fmaxf(fmaxf(top[0][0], top[0][1]), fmaxf(top[0][2], top[0][3]));
     m2 = fmaxf(fmaxf(top[1][0], top[1][1]), fmaxf(top[1][2], top[1][3]));
-    const bool sees = ml[0] != -INFINITY;  // (both maps see the same keys; the sums of a part that sees none were not written)
-    const float f1 = sees ? __builtin_amdgcn_exp2f(ml[0] - m1) : 0.f, f2 = sees ? __builtin_amdgcn_exp2f(ml[2] - m2) : 0.f;
+    const bool written = ml[0] != -INFINITY || ml[2] != -INFINITY;
+    const float f1 = diff_join_factor(ml[0], m1), f2 = diff_join_factor(ml[2], m2);
     float l1 = wave_sum(ml[1] * f1), l2 = wave_sum(ml[3] * f2);
-    factor[0][threadIdx.x] = sees ? f1 : -1.f;
-    factor[1][threadIdx.x] = sees ? f2 : -1.f;
+    factor[0][threadIdx.x] = written ? f1 : -1.f;
+    factor[1][threadIdx.x] = written ? f2 : -1.f;
     if (lane == 0) {
         total[0][wave] = l1;
         total[1][wave] = l2;

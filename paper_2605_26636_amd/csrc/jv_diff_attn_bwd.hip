@@ -11,7 +11,7 @@ namespace jv {
 
 // What both passes need of a query, from the rows of O and P2 V that the forward pass left in the element type
 // (P1 V = O + lambda P2 V) and its references and sums: a.stats holds
-//     [0], [1]   -log2(denominator of map m) / c, which a score product starts from: the weight is 2^(c sum), 0 for a row that sees no key
+//     [0], [1]   -log2(denominator of map m) / c, which a score product starts from: the weight is 2^(c sum), 0 in a map without a weight
 //     [2]        -D1            [3]   -lambda (D1 - D2),    Dm = rowsum(dO o (Pm V)),
 // and for fp32 tensors, whose weights e inv with e = 2^(c score - m) keep the reference m and the sum 1 / inv apart (their logarithm, rounded, would
 // cost the weights 2^-24 of its size),
@@ -59,20 +59,21 @@ __global__ void __launch_bounds__(256) diff_attn_rows_kernel(DiffArgs a) {
     if (!live || ch >= STATS * PER) return;
     const long long n = diff_rows(a);
     const int which = ch / PER;  // a statistic a lane
-    const float m1 = qi < DiffLengths(a, b).q ? a.ml[row] : INFINITY;  // (both maps see the same keys)
+    const int map = sizeof(T) == 2 ? which & 1 : which < 2 ? which : which < 4 ? 0 : 1;  // whose reference and sum it is made of
+    const float m = qi < DiffLengths(a, b).q ? a.ml[2 * map * n + row] : INFINITY, l = a.ml[(2 * map + 1) * n + row];  // m = +inf: no weight in this map
     float stat;
     if constexpr (sizeof(T) == 2) {
         if (which == 2) stat = -d1;
         else if (which == 3) stat = -lam * (d1 - d2);
-        else stat = m1 == INFINITY ? -INFINITY : -(a.ml[2 * which * n + row] + log2f(a.ml[(2 * which + 1) * n + row])) / a.c;
-    } else if (m1 == INFINITY) {
-        stat = which < 2 ? -INFINITY : 0.f;
-    } else if (which < 2) {
-        stat = -a.ml[2 * which * n + row];
+        else stat = m == INFINITY ? -INFINITY : -(m + log2f(l)) / a.c;
     } else if (which == 6) {
         stat = d2;
+    } else if (m == INFINITY) {
+        stat = which < 2 ? -INFINITY : 0.f;
+    } else if (which < 2) {
+        stat = -m;
     } else {
-        const float inv = 1.f / a.ml[(which < 4 ? 1 : 3) * n + row];
+        const float inv = 1.f / l;
         stat = inv * (which == 2 ? 1.f : which == 3 ? -d1 : which == 4 ? -lam : lam * d2);
     }
     a.stats[which * n + row] = stat;
@@ -97,8 +98,8 @@ struct DiffRowGrad {
         const long long n = diff_rows(a);
         minus_m1 = -a.ml[row];
         minus_m2 = -a.ml[2 * n + row];
-        f1 = 1.f / a.ml[n + row];
-        inv2 = 1.f / a.ml[3 * n + row];
+        f1 = minus_m1 == -INFINITY ? 0.f : 1.f / a.ml[n + row];  // (a map without a weight)
+        inv2 = minus_m2 == -INFINITY ? 0.f : 1.f / a.ml[3 * n + row];
         const float minus_d1 = a.stats[2 * n + row], lam_d2 = a.stats[3 * n + row] - lam * minus_d1;
         h1 = minus_d1 * f1;
         f2 = -lam * inv2;
