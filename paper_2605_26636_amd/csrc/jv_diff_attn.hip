@@ -251,18 +251,21 @@ __device__ inline float diff_exp_pack(DiffWeights<TERMS> &w, const f32x16 &s, fl
     return sum0 + sum1;
 }
 template <int W, int TERMS>
+__device__ inline float diff_raise_pack(DiffMap<W> &w, DiffWeights<TERMS> &p, const f32x16 &s, float c) {
+    const float ref = diff_raise<W>(w, s, c);
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < 8; ++v) {
+        const float p0 = diff_weight(s[2 * v], c, ref), p1 = diff_weight(s[2 * v + 1], c, ref);
+        p.set(v, p0, p1);
+        sum += p0 + p1;
+    }
+    return sum;
+}
+template <int W, int TERMS>
 __device__ inline void diff_softmax_pack(DiffMap<W> &w, DiffWeights<TERMS> &p, const f32x16 &s, float c) {
     float sum = diff_exp_pack(p, s, c, w.minus_m);
-    if (__builtin_amdgcn_ballot_w64(!(sum <= kDiffLazySum)) != 0) {
-        const float ref = diff_raise<W>(w, s, c);
-        sum = 0.f;
-#pragma unroll
-        for (int v = 0; v < 8; ++v) {
-            const float p0 = diff_weight(s[2 * v], c, ref), p1 = diff_weight(s[2 * v + 1], c, ref);
-            p.set(v, p0, p1);
-            sum += p0 + p1;
-        }
-    }
+    if (__builtin_amdgcn_ballot_w64(!(sum <= kDiffLazySum)) != 0) sum = diff_raise_pack(w, p, s, c);
     w.l += sum;
 }
 
@@ -340,7 +343,29 @@ __global__ void __launch_bounds__(64 * WAVES, W == 128 && WAVES == 1 ? 1 : 2) di
         if ((tile + 1) * kDiffTile > least) diff_hide_keys(s1, s2, tile * kDiffTile, limit, g);
         constexpr int TERMS = BOTH ? 2 : 1;
         DiffWeights<TERMS> p1, p2;
-        diff_softmax_pack(w1, p1, s1, a.c);
+        if (BOTH) {
+            float sum = diff_exp_pack(p1, s1, a.c, w1.minus_m);
+            if (__builtin_amdgcn_ballot_w64(!(sum <= kDiffLazySum)) != 0) {
+                // Zeros times what is not finite in a key's other half are NaN: the maps' scores apart then (and where a masked tile is tried without a reference).
+                if (__builtin_amdgcn_ballot_w64(sum != sum) != 0) {
+                    f32x16 t1, t2;
+                    diff_zero(t1);
+                    diff_zero(t2);
+#pragma unroll
+                    for (int ks = 0; ks < KS; ++ks) {
+                        t1 = mfma32(as_bf16x8(k1[ks]), q[ks], t1);
+                        t2 = mfma32(as_bf16x8(k2[ks]), q[KS + ks], t2);
+                    }
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) s1[v] = li < 16 ? t1[v] : t2[v];
+                    if ((tile + 1) * kDiffTile > least) diff_hide_keys(s1, s2, tile * kDiffTile, limit, g);
+                }
+                sum = diff_raise_pack(w1, p1, s1, a.c);
+            }
+            w1.l += sum;
+        } else {
+            diff_softmax_pack(w1, p1, s1, a.c);
+        }
         u32x2 v0[2 * CB];
         Lds::template read_cols<TILE, 0>(v0, vat);
         __builtin_amdgcn_sched_barrier(0);

@@ -104,3 +104,25 @@ def test_a_map_whose_logits_all_overflow_weighs_nothing(dtype, W, heads, n_q):
                 rel = np.linalg.norm(got - ref[n]) / np.linalg.norm(ref[n])
                 print(n_k, m, n, rel, flush=True)
                 assert rel <= tol, (n_k, m, n)
+
+
+@pytest.mark.parametrize("heads,n_q", ROWS)
+@pytest.mark.parametrize("at", [2, "second map"])
+@pytest.mark.parametrize("W", [64, 128])
+def test_infinity_in_a_key_of_bf16_tensors(W, at, heads, n_q):
+    """It makes a logit of +inf, which is NaN, or of -inf, which takes no part in its map and does not touch the other: by the sign of the query's number."""
+    at = W // 2 + 2 if at == "second map" else at
+    for n_k in KEYS:
+        for key in {0, n_k // 2, n_k - 1}:
+            x = D.make(n_k + W, 1, heads, 1, n_q, n_k, W, "bf16")
+            near = x["q"][..., at].abs() < 0.25
+            x["q"][..., at][near] = -0.25
+            nan = D.host(x["q"])[..., at] > 0
+            # a logit of -256 / sqrt(W / 2) or less weighs 2^-46 of the others at most
+            x["k"][0, 0, key, at] = 2.0 ** 10
+            want = D.Bounds(x, "bf16")
+            x["k"][0, 0, key, at] = float("inf")
+            got = D.host(D.run(x)["o"])
+            assert np.isnan(got[nan]).all(), (n_k, key)
+            assert np.isfinite(got[~nan]).all(), (n_k, key)
+            D.Bounds.one(f"{n_k} {key}", np.where(nan[..., None], want.o, got), want.o, want.off["o"])
