@@ -121,9 +121,10 @@ struct DiffRowGrad {
     }
 };
 
-// dQ of a wavefront's queries, or its part of it, and the workgroup's sum of P2 o dP.
+// dQ of a wavefront's queries, or its part of it, and the workgroup's sum of P2 o dP.  Queries that see no key went along with weights of zero, which
+// K and V that are not finite turn into NaN: zeros are written for them.
 template <typename T, int W>
-__device__ inline void diff_finish_dq(const DiffArgs &a, const f32x16 (&acc)[W / 32], float lam_sum, int b, int h, int block, int part, float (&wave_lam)[4], int tid) {
+__device__ inline void diff_finish_dq(const DiffArgs &a, const f32x16 (&acc)[W / 32], float lam_sum, bool sees, int b, int h, int block, int part, float (&wave_lam)[4], int tid) {
     const int lane = tid & 63, g = lane >> 5, wave = tid >> 6, qi = (block * 4 + wave) * 32 + (lane & 31);
     const long long bh = (long long)b * a.heads + h;
     if (qi < a.n_q) {
@@ -134,13 +135,15 @@ __device__ inline void diff_finish_dq(const DiffArgs &a, const f32x16 (&acc)[W /
 #pragma unroll
             for (int q4 = 0; q4 < 4; ++q4) {
                 const f32x16 &x = acc[cb];
-                const f32x4 y = {x[4 * q4] * a.scale, x[4 * q4 + 1] * a.scale, x[4 * q4 + 2] * a.scale, x[4 * q4 + 3] * a.scale};
+                f32x4 y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = sees ? x[4 * q4 + e] * a.scale : 0.f;
                 const int ch = 32 * cb + 8 * q4 + 4 * g;
                 if (a.parts > 1) diff_store4(partial + ch, y);
                 else diff_store4(dq + ch, y);
             }
     }
-    lam_sum = wave_sum(lam_sum);
+    lam_sum = wave_sum(sees ? lam_sum : 0.f);
     if (lane == 0) wave_lam[wave] = lam_sum;
     __syncthreads();
     if (tid == 0) a.lam_part[(bh * a.blocks + block) * a.parts + part] = (wave_lam[0] + wave_lam[1]) + (wave_lam[2] + wave_lam[3]);
@@ -303,7 +306,7 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dq_bf16_kernel(DiffArgs a) {
         lds_barrier();
     }
     asm("" : "+v"(lam_sum));
-    diff_finish_dq<__bf16, W>(a, acc, lam_sum * r.inv2, p.b, p.h, p.block, p.part, wave_lam, tid);
+    diff_finish_dq<__bf16, W>(a, acc, lam_sum * r.inv2, p.limit > 0, p.b, p.h, p.block, p.part, wave_lam, tid);
 }
 
 // The same for fp32 tensors, on operands of three bf16 numbers.  For lambda D2 is added up, once a row: the matrix unit's dP, a sum of so many small
@@ -398,7 +401,7 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dq_f32_kernel(DiffArgs a) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the next tile, for every wavefront, and every wavefront done with this one
         lds_barrier();
     }
-    diff_finish_dq<float, W>(a, acc, p.part == 0 && g == 0 ? r.d2 : 0.f, p.b, p.h, p.block, p.part, wave_lam, tid);
+    diff_finish_dq<float, W>(a, acc, p.part == 0 && g == 0 ? r.d2 : 0.f, p.limit > 0, p.b, p.h, p.block, p.part, wave_lam, tid);
 }
 
 // Where a workgroup of the key pass stands: 128 keys of a kv head; the tiles of its group's heads, one head after the other, of

@@ -126,3 +126,19 @@ def test_infinity_in_a_key_of_bf16_tensors(W, at, heads, n_q):
             assert np.isnan(got[nan]).all(), (n_k, key)
             assert np.isfinite(got[~nan]).all(), (n_k, key)
             D.Bounds.one(f"{n_k} {key}", np.where(nan[..., None], want.o, got), want.o, want.off["o"])
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("dtype,W", KINDS)
+def test_rows_that_see_no_key_stay_zero_beside_rows_that_are_nan(dtype, W, value):
+    """Queries behind a sequence's end, and causal ones in front of all keys, beside a key or a value that is not finite."""
+    for causal, lengths, n_q, n_k in ((False, ([20, 0], [50, 50]), 45, 50), (True, (None, None), 150, 40), (False, (None, [0, 300]), 40, 300)):
+        for n in ("k", "v"):
+            x = D.make(32, 2, 2, 1, n_q, n_k, W, dtype)
+            x[n][:, :, 3, 7] = value
+            out = D.run(x, causal=causal, lengths=lengths, backward=True, d_lam=False)
+            keep = [diff.visible(n_q, n_k, causal, *(None if l is None else l[b] for l in lengths)).any(1) for b in range(2)]
+            assert not all(x.all() for x in keep)
+            for b in range(2):
+                for t in ("o", "q"):
+                    assert not out[t][b][:, ~torch.from_numpy(keep[b])].cpu().float().abs().nan_to_num(1.0).any(), (causal, n, t, b)
