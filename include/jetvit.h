@@ -331,8 +331,9 @@ jv_status jv_diff_attn_fwd(const jv_diff_attn_desc *desc, const void *q, const v
  *     dQm = scale dSm Km,   dKm = scale dSm^T Qm,   dlambda_h = - sum P2 o dP,
  * dK and dV summed over the heads that share them.  d_q1 .. d_k2 receive the gradients of lambda's vectors in fp32, in their
  * layout (summed over the heads where these share one set); all four, or none (NULL).
- * The weights are formed again: for dK and dV of JV_BF16 from the logarithm of their denominators, in fp32, off by 2^-24 of the
- * logit's size, so that logits beyond 2^20 leave no gradient of use (the forward pass takes any that are finite).
+ * The weights are formed again, from scores of the forward pass's bits: for d_q, the gradients of lambda's vectors and all of JV_F32 as the forward
+ * pass formed them, at logits of any finite size; for dK and dV of JV_BF16 from the logarithm of their denominators, in fp32, off by
+ * 2^-24 of the logit's size, so that logits beyond 2^20 leave no dK and dV of use.
  * Outputs in one place (d_k = d_v, say) are not looked for: each needs memory of its own.
  * Sums have a fixed order (no atomics): the same call gives the same bits.  Rows of d_q, d_k, d_v may not overlap; d_q, d_k, d_v may be views of
  * one buffer that lie between each other's rows. */

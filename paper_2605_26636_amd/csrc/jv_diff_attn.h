@@ -208,6 +208,15 @@ __device__ inline f32x16 diff_mma6(const bf16x8 (&a)[3], const bf16x8 (&b)[3], f
     c = mfma32(a[0], b[1], c);
     return mfma32(a[0], b[0], c);
 }
+// The bits of diff_mma6(b, a, c)'s transpose.
+__device__ inline f32x16 diff_mma6_swapped(const bf16x8 (&a)[3], const bf16x8 (&b)[3], f32x16 c) {
+    c = mfma32(a[0], b[2], c);
+    c = mfma32(a[2], b[0], c);
+    c = mfma32(a[1], b[1], c);
+    c = mfma32(a[0], b[1], c);
+    c = mfma32(a[1], b[0], c);
+    return mfma32(a[0], b[0], c);
+}
 // Leading parts of two numbers packed, and what is left of them.
 __device__ inline unsigned diff_take_pair(float &x, float &y) {
     const unsigned u = __builtin_bit_cast(unsigned, x), v = __builtin_bit_cast(unsigned, y);
@@ -238,6 +247,7 @@ __device__ inline DiffPlanes diff_global_planes(const __bf16 *row, int ks, int g
 }
 __device__ inline void diff_landed(u32x4 (&x)[3]) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2])); }
 __device__ inline void diff_landed(u32x4 (&x)[3], u32x4 &y) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(y)); }
+__device__ inline void diff_landed(u32x4 (&x)[3], unsigned &y) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(y)); }
 __device__ inline void diff_landed(u32x2 (&x)[6]) {
     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]));
 }

@@ -184,6 +184,18 @@ struct DiffQueries {
     }
 };
 
+// A reference whose neighbours are whole units of log2 away: the forward pass rounded the product that it was taken from, and so does what forms a weight from
+// it again (against an exact product the weight is off by up to 2^(|m| 2^-24), which overflows in the end): scores are scaled
+// first, and are multiplied by one then.  Scores have the forward pass's bits: the same operands in the same order.
+__device__ inline bool diff_far(float minus_m) { return fabsf(minus_m) >= 16777216.f && fabsf(minus_m) < INFINITY; }
+__device__ inline void diff_scale_scores(f32x16 &s1, f32x16 &s2, float c) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        s1[v] *= c;
+        s2[v] *= c;
+    }
+}
+
 // Scores and dP of a tile (rows: keys) become the gradients of the logits, in place; returns the lane's sum of e2 dP.
 // For lambda, bf16 tensors add these up, tile by tile (one sum over 2 048 products was off four times as far): their D2 holds the rounding of P2 V's
 // weights and rows, which shows in a sum of so many signs.  fp32 tensors add up D2 (diff_attn_dq_f32_kernel).
@@ -248,6 +260,8 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dq_bf16_kernel(DiffArgs a) {
 #pragma unroll
     for (int ks = 0; ks < 2 * KS; ++ks) asm volatile("" : "+v"(q[ks]), "+v"(go[ks]));  // (waited for here, not inside the loop)
     asm volatile("" : "+v"(r.minus_m1), "+v"(r.minus_m2), "+v"(r.f1), "+v"(r.h1), "+v"(r.f2), "+v"(r.h2), "+v"(r.inv2));
+    const bool far = __builtin_amdgcn_ballot_w64(diff_far(r.minus_m1) || diff_far(r.minus_m2)) != 0;
+    const float scaled = far ? 1.f : a.c;
     f32x16 acc[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) diff_zero(acc[cb]);
@@ -286,7 +300,8 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dq_bf16_kernel(DiffArgs a) {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) dp = mfma32(as_bf16x8(y[ks]), go[KS + ks], dp);
         if ((tile + 1) * kDiffTile > p.least) diff_hide_keys(s1, s2, tile * kDiffTile, p.limit > 0 ? p.limit : a.n_k + kDiffTile, g);
-        lam_sum += diff_logit_grads(s1, s2, dp, r, a.c);
+        if (far) diff_scale_scores(s1, s2, a.c);
+        lam_sum += diff_logit_grads(s1, s2, dp, r, scaled);
         bf16x8 ds1[2], ds2[2];
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
@@ -347,6 +362,8 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dq_f32_kernel(DiffArgs a) {
     for (int ks = 0; ks < 2 * KS; ++ks)  // (waited for here, not inside the loop)
         asm volatile("" : "+v"(q[ks].x[0]), "+v"(q[ks].x[1]), "+v"(q[ks].x[2]), "+v"(go[ks].x[0]), "+v"(go[ks].x[1]), "+v"(go[ks].x[2]));
     asm volatile("" : "+v"(r.minus_m1), "+v"(r.minus_m2), "+v"(r.f1), "+v"(r.h1), "+v"(r.f2), "+v"(r.h2), "+v"(r.d2));
+    const bool far = __builtin_amdgcn_ballot_w64(diff_far(r.minus_m1) || diff_far(r.minus_m2)) != 0;
+    const float scaled = far ? 1.f : a.c;
     f32x16 acc[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) diff_zero(acc[cb]);
@@ -381,7 +398,8 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dq_f32_kernel(DiffArgs a) {
         diff_read_cols3<W, 0, 0>(v[0], cols, 0);
         __builtin_amdgcn_sched_barrier(0);
         if ((tile + 1) * kDiffTile > p.least) diff_hide_keys(s1, s2, tile * kDiffTile, p.limit > 0 ? p.limit : a.n_k + kDiffTile, g);
-        diff_logit_grads(s1, s2, dp, r, a.c);
+        if (far) diff_scale_scores(s1, s2, a.c);
+        diff_logit_grads(s1, s2, dp, r, scaled);
         diff_landed(v[0]);
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
@@ -733,7 +751,7 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
         diff_zero(dk[cb]);
         diff_zero(dv[cb]);
     }
-    const unsigned rows0 = Lds::rows(lds_address(smem), lane), cols0 = Lds::cols(lds_address(smem), lane), stats0 = lds_address(smem) + 6 * TILE + 16 * g;
+    const unsigned rows0 = Lds::rows(lds_address(smem), lane), cols0 = Lds::cols(lds_address(smem), lane), stats0 = lds_address(smem) + 6 * TILE + 16 * g, refs0 = lds_address(smem) + 6 * TILE + 4 * lane;
     const unsigned vrows = Lds::rows(lds_address(vt), lane);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     lds_barrier();
@@ -741,13 +759,17 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
         if (!LAST && at + 1 < p.to) issue(stage ^ 1);
         const unsigned rows = rows0 + stage * STAGE, cols = cols0 + stage * STAGE, stats = stats0 + stage * STAGE;
         f32x16 s1, s2, dp;
+        bool far;  // a reference of the tile's queries, the first two rows of statistics, one a lane
         diff_zero(s1);
         diff_zero(s2);
         diff_zero(dp);
         {
             u32x4 x[2][3], last[2];
+            unsigned ref;
             diff_read_rows3<W, 0>(x[0], rows, 0);
-            diff_landed(x[0]);
+            asm volatile("ds_read_b32 %0, %1" : "=v"(ref) : "v"(refs0 + stage * STAGE));
+            diff_landed(x[0], ref);
+            far = __builtin_amdgcn_ballot_w64(diff_far(__builtin_bit_cast(float, ref))) != 0;
 #pragma unroll
             for (int i = 0; i < 4 * KS; ++i) {  // Q operands, then dO operands
                 const int next = (i + 1) & 1;
@@ -759,8 +781,8 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
                 __builtin_amdgcn_sched_barrier(0);
                 bf16x8 q[3];
                 diff_rows3(x[i & 1], q);
-                if (i < KS) s1 = diff_mma6(q, k[i < KS ? i : 0].x, s1);
-                else if (i < 2 * KS) s2 = diff_mma6(q, k[i < 2 * KS ? i : 0].x, s2);
+                if (i < KS) s1 = diff_mma6_swapped(q, k[i < KS ? i : 0].x, s1);
+                else if (i < 2 * KS) s2 = diff_mma6_swapped(q, k[i < 2 * KS ? i : 0].x, s2);
                 else {
                     DiffPlanes &y = v[i < 2 * KS ? 0 : i - 2 * KS];
                     if (LAST) {
@@ -778,6 +800,8 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
         }
         if (LAST && at + 1 < p.to) issue(stage ^ 1);  // (not in front of the products above: two operands of theirs come from scratch memory, for which they would wait for the tile too)
         if (p.masked(a, tile)) p.hide(a, s1, s2, tile, g);
+        if (far) diff_scale_scores(s1, s2, a.c);
+        const float scaled = far ? 1.f : a.c;
         // four rows' statistics at a time, the next four's on their way
         {
             u32x4 st[2][6];
@@ -800,7 +824,7 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int r = 4 * q4 + e;
-                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s1[r], a.c, y[0][e])), e2 = __builtin_amdgcn_exp2f(fmaf(s2[r], a.c, y[1][e]));
+                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s1[r], scaled, y[0][e])), e2 = __builtin_amdgcn_exp2f(fmaf(s2[r], scaled, y[1][e]));
                     s1[r] = e1 * fmaf(dp[r], y[2][e], y[3][e]);
                     s2[r] = e2 * fmaf(dp[r], y[4][e], y[5][e]);
                     dp[r] = fmaf(e2, y[4][e], e1 * y[2][e]);
