@@ -8,6 +8,7 @@ goes through ctypes.  Tensors are torch tensors on the GPU (torch is used for de
 and streams); the functions carry the names of the C entry points.  There is no
 CPU fallback: a missing library or a non-OK status raises.
 """
+import contextlib
 import ctypes
 import os
 
@@ -221,6 +222,13 @@ def _stream(stream):
     return ctypes.c_void_p(s.cuda_stream)
 
 
+def _scratch(need, device, stream):
+    """Scratch memory of a call: allocated on the stream that the call runs on, so that, let go of, it is not handed to
+    another stream's tensors while the call still writes to it."""
+    with torch.cuda.stream(stream) if isinstance(stream, torch.cuda.Stream) else contextlib.nullcontext():
+        return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+
+
 def jv_version():
     return lib().jv_version().decode()
 
@@ -234,7 +242,7 @@ def jv_linear_attn_fwd(q, k, v, o, grid, eps=1e-6, workspace=None, stream=None):
     if workspace is None:
         grid = tuple(grid)
         need = jv_linear_attn_workspace_bytes(make_desc(q, k, v, o, grid))
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+        workspace = _scratch(need, q.device, stream)
     st = (_native or _load_native()).linear_attn_fwd(q, k, v, o, grid, eps, workspace, stream)
     if st is None:
         desc = make_desc(q, k, v, o, grid)
@@ -285,7 +293,7 @@ def _linear_block(q, k, v, o, grid, eps, static_kernel, squeeze, ksize, token, f
     if workspace is None:
         grid = tuple(grid)
         need = jv_linear_block_workspace_bytes(make_desc(q, k, v, o, grid), make_dwc_params(static_kernel, squeeze, ksize, token))
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+        workspace = _scratch(need, q.device, stream)
     st = (_native or _load_native()).linear_block_fwd(q, k, v, o, grid, eps, static_kernel, squeeze, ksize, token,
                                                       focus_p, workspace, stream)
     if st is None:
@@ -400,7 +408,7 @@ def jv_diff_attn_fwd(q, k, v, lam, o, lambda_init=0.8, scale=0.0, causal=False, 
     jv_diff_attn_saved_bytes bytes that receives what the gradient needs.  Returns the workspace tensor used."""
     if workspace is None:
         desc = make_diff_desc(q, k, v, o, causal, q_lengths, k_lengths)
-        workspace = torch.empty(max(jv_diff_attn_workspace_bytes(desc), 256), dtype=torch.uint8, device=q.device)
+        workspace = _scratch(jv_diff_attn_workspace_bytes(desc), q.device, stream)
     st = (_native or _load_native()).diff_attn_fwd(q, k, v, lam, o, lambda_init, scale, causal, q_lengths, k_lengths, saved, workspace, stream)
     if st is None:
         desc = make_diff_desc(q, k, v, o, causal, q_lengths, k_lengths)
@@ -417,7 +425,7 @@ def jv_diff_attn_bwd(q, k, v, lam, o, saved, d_o, d_q, d_k, d_v, d_lam=None, lam
     are given as they were there; returns the workspace tensor used."""
     if workspace is None:
         desc = make_diff_desc(q, k, v, o, causal, q_lengths, k_lengths)
-        workspace = torch.empty(max(jv_diff_attn_bwd_workspace_bytes(desc), 256), dtype=torch.uint8, device=q.device)
+        workspace = _scratch(jv_diff_attn_bwd_workspace_bytes(desc), q.device, stream)
     st = (_native or _load_native()).diff_attn_bwd(q, k, v, lam, o, saved, d_o, d_q, d_k, d_v, d_lam, lambda_init, scale, causal, q_lengths,
                                                    k_lengths, workspace, stream)
     if st is None:
@@ -489,7 +497,7 @@ def jv_layernorm_bwd(x, gamma, dy, dx, dgamma=None, dbeta=None, eps=1e-6, residu
     Returns the workspace tensor used."""
     rows, cols = x.shape
     if workspace is None:
-        workspace = torch.empty(max(jv_layernorm_bwd_workspace_bytes(rows, cols), 256), dtype=torch.uint8, device=x.device)
+        workspace = _scratch(jv_layernorm_bwd_workspace_bytes(rows, cols), x.device, stream)
     st = (_native or _load_native()).layernorm_bwd(x, gamma, dy, dx, dgamma, dbeta, eps, residual, workspace, stream)
     if st is None:
         _same_device(x, gamma, dy, dx, dgamma, dbeta, residual, workspace)
@@ -591,7 +599,7 @@ class Encoder:
         if x.dtype != sd or y.dtype != sd or not x.is_contiguous() or not y.is_contiguous():
             raise ValueError("x and y must be contiguous tensors of the stream's element type")
         if workspace is None:
-            workspace = torch.empty(self.workspace_bytes(batch, grid), dtype=torch.uint8, device=x.device)
+            workspace = _scratch(self.workspace_bytes(batch, grid), x.device, stream)
         if not taps:
             _check(lib().jv_encoder_forward(self._handle, x.data_ptr(), y.data_ptr(), batch, grid[0],
                                             grid[1], workspace.data_ptr(), workspace.numel(),

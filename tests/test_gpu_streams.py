@@ -1,5 +1,5 @@
 """Calls on a stream of their own: work goes there in the order in which it was given, whatever the current stream is and however a call is
-marshalled."""
+marshalled, and scratch memory that a call takes for itself stays the stream's."""
 import pytest
 import torch
 
@@ -109,3 +109,42 @@ def test_a_step_on_a_side_stream_and_captured_from_it():
     for _ in range(3):
         graph.replay()
         same()
+
+
+@pytest.mark.parametrize("call", ["forward", "backward", "norm", "linear", "block"])
+def test_scratch_that_a_call_takes_for_itself_stays_its_stream_s(call):
+    """A call on a named stream allocates its scratch there: let go of while the call waits its turn, the memory does not come back to the current
+    stream, whose next tensors would be written over."""
+    side = torch.cuda.Stream()
+    x = D.make(45, 2, 4, 2, 70, 900, 64, "fp32")
+    q, k, v, d_o = (x[n].cuda() for n in ("q", "k", "v", "d_o"))
+    lam = tuple(t.cuda() for t in x["lam"])
+    o, dq, dk, dv = (torch.empty_like(t) for t in (q, q, k, v))
+    saved = torch.empty(binding.jv_diff_attn_saved_bytes(binding.make_diff_desc(q, k, v, o)), dtype=torch.uint8, device="cuda")
+    rows, gamma = torch.randn(700, 256).cuda(), torch.ones(256, device="cuda")
+    out, dgamma, dbeta = torch.empty_like(rows), torch.empty_like(gamma), torch.empty_like(gamma)
+    grid = (30, 30)
+    binding.jv_diff_attn_fwd(q, k, v, lam, o, saved=saved)
+
+    def run(stream):
+        if call == "forward":
+            return binding.jv_diff_attn_fwd(q, k, v, lam, o, stream=stream), o
+        if call == "backward":
+            return binding.jv_diff_attn_bwd(q, k, v, lam, o, saved, d_o, dq, dk, dv, stream=stream), dk
+        if call == "norm":
+            return binding.jv_layernorm_bwd(rows, gamma, rows, out, dgamma, dbeta, stream=stream), dgamma
+        if call == "linear":
+            return binding.jv_linear_attn_fwd(k, k, v, dk, grid, stream=stream), dk
+        return binding.jv_linear_block_fwd(k, k, v, dk, grid, static_kernel=torch.ones(128, 3, 3, device="cuda"), stream=stream), dk
+    want = run(None)[1].clone()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    waiting(side)
+    ws, got = run(side)
+    at, n = ws.data_ptr(), ws.numel()
+    del ws
+    mine = [torch.full((n,), 0xff, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    assert all(t.data_ptr() != at for t in mine)
+    side.synchronize()
+    assert torch.equal(got, want)
+    assert all(bool((t == 0xff).all()) for t in mine)
