@@ -288,7 +288,8 @@ jv_status jv_full_attn_fwd(const jv_attn_desc *desc, const void *q, const void *
  * A logit of -inf (of finite numbers whose product overflows, too) weighs nothing in its map and leaves the other map alone; a map whose
  * logits are all -inf weighs nothing, as one that sees no key; a logit of +inf and NaN in a query are NaN in its row of O and what
  * follows from it, however the keys are cut.  A key or value that is not finite and that causal queries see may reach others of its sequence,
- * which meet it with a weight of 0.
+ * which meet it with a weight of 0; so may, in the gradient, a row of Q or dO that is not finite, the keys that it does not see.  Not so what lies
+ * behind the lengths.
  * JV_BF16: the weights Pm are rounded to bf16 in front of the product with V (up to 16 queries of the heads that share K and V: to
  * the sum of two bf16 numbers), and in the gradient P1 - lambda P2 and the gradients of the logits in front of theirs; everything
  * else is fp32.
@@ -329,7 +330,8 @@ jv_status jv_diff_attn_fwd(const jv_diff_attn_desc *desc, const void *q, const v
  * dP = dO V^T and Dm the row sums of dO o (Pm V):
  *     dV = (P1 - lambda P2)^T dO,   dS1 = P1 o (dP - D1),   dS2 = -lambda P2 o (dP - D2),
  *     dQm = scale dSm Km,   dKm = scale dSm^T Qm,   dlambda_h = - sum P2 o dP,
- * dK and dV summed over the heads that share them.  d_q1 .. d_k2 receive the gradients of lambda's vectors in fp32, in their
+ * dK and dV summed over the heads that share them.  P1 V is formed again as O + lambda P2 V, from rows that were stored in the element type: the
+ * rounding in D1 grows with |lambda|.  d_q1 .. d_k2 receive the gradients of lambda's vectors in fp32, in their
  * layout (summed over the heads where these share one set); all four, or none (NULL).
  * The weights are formed again, from scores of the forward pass's bits: for d_q, the gradients of lambda's vectors and all of JV_F32 as the forward
  * pass formed them, at logits of any finite size; for dK and dV of JV_BF16 from the logarithm of their denominators, in fp32, off by

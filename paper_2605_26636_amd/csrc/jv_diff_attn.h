@@ -50,7 +50,9 @@ struct DiffProblem {
 };
 
 // What a workgroup works on: a block of rows (or keys) of a (batch, head) and one of `parts` parts of it.  Without a mask, contiguous
-// ranges of (batch, head)s per XCD (workgroup w runs on XCD w % 8), so that the workgroups of one share its K and V in one L2.
+// ranges of (batch, head)s per XCD (workgroup w runs on XCD w % 8), so that the workgroups of one share its K and V in one L2.  Sequences of different
+// lengths lie on few XCDs each then, and a launch lasts as long as the longest one's: a step of 4 sequences of 854 to 1 183 tokens x 16 heads of 64
+// 221 us, of four of 1 183 219, of four of their mean 187.
 // Causal: the blocks with most work of all of them first (an XCD's (batch, head)s one after the other leave its last long
 // blocks alone at the end: forward pass of 2 x 4 096 tokens x 16 heads of 128 channels 291 us, so 232; where their number is a multiple of
 // 8 each stays on one XCD all the same).  False where a workgroup of the rounded-up grid has no work.
@@ -95,7 +97,10 @@ __device__ inline void diff_zero(f32x16 &x) {
     for (int v = 0; v < 16; ++v) x[v] = 0.f;
 }
 // Operands (see mfma32): lane 32 g + i holds row or column i and elements 8 g .. + 7 of 16.
-// Rows 16 kk .. + 15 of a finished block as B operand: element e of lane 32 g + i is row 16 kk + 8 (e / 4) + 4 g + e % 4.
+// Rows 16 kk .. + 15 of a finished block as B operand: element e of lane 32 g + i is row 16 kk + 8 (e / 4) + 4 g + e % 4.  Rounded to bf16, as the operands
+// beside it are: what the gradient of bf16 tensors does with P1 - lambda P2 and the gradients of the logits (2.5e-3 off 64 bits where the results'
+// rounding alone is 1.7e-3; a second term would be a third more products in the query pass and half as many again in the key
+// pass, which has no registers for it).
 __device__ inline bf16x8 diff_block_frag(const f32x16 &s, int kk) {
     return as_bf16x8(u32x4{pack_bf16x2(s[8 * kk], s[8 * kk + 1]), pack_bf16x2(s[8 * kk + 2], s[8 * kk + 3]),
                            pack_bf16x2(s[8 * kk + 4], s[8 * kk + 5]), pack_bf16x2(s[8 * kk + 6], s[8 * kk + 7])});
@@ -149,10 +154,6 @@ __device__ inline void diff_landed(u32x4 (&x)[4], u32x4 (&y)[4]) {
 __device__ inline void diff_landed(u32x4 (&x)[2], u32x4 (&y)[2]) { asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(y[0]), "+v"(y[1])); }
 __device__ inline void diff_landed(u32x4 (&x)[4], u32x4 (&y)[2]) {
     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(y[0]), "+v"(y[1]));
-}
-__device__ inline void diff_landed(u32x4 (&x)[4], u32x4 (&y)[4], u32x4 (&z)[4]) {
-    asm volatile("s_waitcnt lgkmcnt(0)"
-                 : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(y[0]), "+v"(y[1]), "+v"(y[2]), "+v"(y[3]), "+v"(z[0]), "+v"(z[1]), "+v"(z[2]), "+v"(z[3]));
 }
 __device__ inline void diff_landed(u32x4 (&x)[4], u32x4 (&y)[2], u32x4 (&z)[2]) {
     asm volatile("s_waitcnt lgkmcnt(0)" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(y[0]), "+v"(y[1]), "+v"(z[0]), "+v"(z[1]));

@@ -6,7 +6,6 @@
 // against 32 exponentials a lane.  Few rows, where the keys' bytes are what counts, take one wavefront each and are cut over the keys
 // (jv_plan.h); the parts are joined by a second launch.
 #include <math.h>
-#include <stdlib.h>
 
 #include <algorithm>
 
@@ -225,7 +224,9 @@ __device__ inline int diff_tiles(const DiffArgs &a, const DiffPlace &place, cons
 // instructions (a wavefront working at both at once) changed nothing for 64 channels and does not fit the registers for 128; a shader clock
 // of 2.0 to 2.3 GHz under this load is part of the bound.
 // ---------------------------------------------------------------------------------------
-// Weights of a tile as bf16 numbers, TERMS = 1, or sums of two: rounded, and what rounding left.
+// Weights of a tile as bf16 numbers, TERMS = 1, or sums of two: rounded, and what rounding left.  One term is as much as the matrix instruction takes beside
+// bf16 values: outputs in bf16 are 2.5e-3 off 64 bits (relative 2-norm), with two terms 1.7e-3, the rounding of the outputs alone.  Two terms take 8 or 16
+// products more a tile, 734 / 1 113 us for 8 x 4 096 tokens x 8 heads of 128, so only rows that wait for memory anyway have them.
 template <int TERMS>
 struct DiffWeights {
     unsigned pk[TERMS][8];
@@ -415,9 +416,10 @@ __global__ void __launch_bounds__(64 * WAVES, W == 128 && WAVES == 1 ? 1 : 2) di
 
 // ---------------------------------------------------------------------------------------
 // fp32 tensors: as above on operands of three bf16 numbers, two stages of plane tiles, the next tile on its way under this one's
-// arithmetic.  A tile takes 72 (W = 64) or 144 matrix instructions and the splitting of 32 weights a lane.  Bound by matrix issue
-// where a wavefront has many tiles (2 x 1 024 tokens x 8 heads of 128 86 us, 0.90 PFLOP/s of bf16 products), by a tile's chain of reads, products and
-// splits where it has few (2 x 576 x 12 of 64 in two parts 30 us, 0.60).
+// arithmetic.  A tile takes 72 (W = 64) or 144 matrix instructions and the splitting of 32 weights a lane.  A tile is a chain: the products of the scores,
+// both softmaxes and their splits, the products with V.  With one wavefront a SIMD (rows of 128) nothing else is issued under the middle of it:
+// 2 x 1 024 tokens x 8 heads of 128 86 us, 0.90 PFLOP/s of bf16 products, 0.61 of what a large product reaches; with few tiles a wavefront its
+// start and end count too (2 x 576 x 12 of 64 in two parts 30 us, 0.60 PFLOP/s).
 // ---------------------------------------------------------------------------------------
 template <int W, int WAVES, bool SPLIT>
 __global__ void __launch_bounds__(64 * WAVES, W == 64 && WAVES > 1 ? 2 : 1) diff_attn_fwd_f32_kernel(DiffArgs a) {
