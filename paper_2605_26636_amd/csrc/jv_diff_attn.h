@@ -386,6 +386,15 @@ __device__ inline float diff_lambda_of(const DiffArgs &a, int first, int last, i
     return lam;
 }
 
+// A weight of a score s is 2^(s c - m), the product exact and the reference m rounded, in every tile and in both passes: what the rounding costs is one factor
+// of a row's weights and of their sum.  It is up to 2^(|m| 2^-24): from |m| = 2^24 on products are rounded as the reference was.  Both by the same
+// instruction, (s first) then - m: (s c) 1 - m there, (s 1) c - m below.
+__device__ inline bool diff_far(float m) { return fabsf(m) >= 16777216.f && fabsf(m) < INFINITY; }
+struct DiffScaling {
+    float first, then;
+    __device__ DiffScaling(float c, bool far) : first(far ? c : 1.f), then(far ? 1.f : c) {}
+};
+
 // Four consecutive channels of an output row.
 __device__ inline void diff_store4(float *p, f32x4 x) { *(f32x4 *)p = x; }
 __device__ inline void diff_store4(__bf16 *p, f32x4 x) { *(u32x2 *)p = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])}; }

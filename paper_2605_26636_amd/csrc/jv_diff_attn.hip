@@ -63,14 +63,14 @@ __device__ inline float diff_raise(DiffMap<W> &w, const f32x16 &s, float c) {
             asm volatile("v_mul_f32 %0, %0, %1" : "+v"(x) : "v"(alpha));
             w.acc[cb][v] = x;
         }
-    w.minus_m = fabsf(m_new) < 16777216.f ? -m_new : INFINITY;  // (so large that products must be rounded first: no tile is tried; NaN too)
+    w.minus_m = fabsf(m_new) < 16777216.f ? -m_new : INFINITY;  // (diff_far: no tile is tried; NaN neither)
     return m_new == -INFINITY ? 0.f : m_new;
 }
-// A weight from a rounded product, whose maximum the reference is (from an exact one it could be 2^(|m| 2^-24)).
-__device__ inline float diff_weight(float s, float c, float ref) {
+// A weight against a reference that was just raised (see DiffScaling).
+__device__ inline float diff_weight(float s, float c, float ref, bool far) {
 #pragma clang fp contract(off)
     const float x = s * c;
-    return __builtin_amdgcn_exp2f(x - ref);
+    return __builtin_amdgcn_exp2f(far ? x - ref : fmaf(s, c, -ref));
 }
 // Weights of a tile against the present reference, which is raised only where they come out large (numerator and denominator always
 // use the same one).  Without a reference minus_m is +inf, so every tile raises until a key is seen; where all is masked (s = -inf)
@@ -80,10 +80,11 @@ __device__ inline void diff_softmax(DiffMap<W> &w, f32x16 &p, const f32x16 &s, f
     float sum = diff_exp(p, s, c, w.minus_m);
     if (__builtin_amdgcn_ballot_w64(!(sum <= kDiffLazySum)) != 0) {
         const float ref = diff_raise<W>(w, s, c);
+        const bool far = w.minus_m == INFINITY;
         sum = 0.f;
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-            p[v] = diff_weight(s[v], c, ref);
+            p[v] = diff_weight(s[v], c, ref, far);
             sum += p[v];
         }
     }
@@ -254,10 +255,11 @@ __device__ inline float diff_exp_pack(DiffWeights<TERMS> &w, const f32x16 &s, fl
 template <int W, int TERMS>
 __device__ inline float diff_raise_pack(DiffMap<W> &w, DiffWeights<TERMS> &p, const f32x16 &s, float c) {
     const float ref = diff_raise<W>(w, s, c);
+    const bool far = w.minus_m == INFINITY;
     float sum = 0.f;
 #pragma unroll
     for (int v = 0; v < 8; ++v) {
-        const float p0 = diff_weight(s[2 * v], c, ref), p1 = diff_weight(s[2 * v + 1], c, ref);
+        const float p0 = diff_weight(s[2 * v], c, ref, far), p1 = diff_weight(s[2 * v + 1], c, ref, far);
         p.set(v, p0, p1);
         sum += p0 + p1;
     }

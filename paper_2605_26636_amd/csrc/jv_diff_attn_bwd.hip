@@ -85,10 +85,12 @@ __device__ inline void diff_part(const DiffArgs &a, int part, int total, int *fr
     *to = (unsigned)total * (part + 1) / (unsigned)a.parts;
 }
 
-// What the query pass knows of a query: its weights are e inv with e = 2^(c score - m), and the gradients of its logits
+// What the query pass knows of a query: its weights are e inv with e = 2^(c score - m), formed as the forward pass did (DiffScaling; scores have its
+// bits: the same operands in the same order), and the gradients of its logits
 // dS1 = e1 (dP f1 + h1), dS2 = e2 (dP f2 + h2).
 struct DiffRowGrad {
     float minus_m1, minus_m2, f1, h1, f2, h2;
+    float c1, c2;  // DiffScaling::then
     float inv2;  // bf16 tensors
     float d2;    // fp32 tensors
     __device__ void load(const DiffArgs &a, long long row, bool sees, float lam) {
@@ -184,26 +186,22 @@ struct DiffQueries {
     }
 };
 
-// A reference whose neighbours are whole units of log2 away: the forward pass rounded the product that it was taken from, and so does what forms a weight from
-// it again (against an exact product the weight is off by up to 2^(|m| 2^-24), which overflows in the end): scores are scaled
-// first, and are multiplied by one then.  Scores have the forward pass's bits: the same operands in the same order.
-__device__ inline bool diff_far(float minus_m) { return fabsf(minus_m) >= 16777216.f && fabsf(minus_m) < INFINITY; }
-__device__ inline void diff_scale_scores(f32x16 &s1, f32x16 &s2, float c) {
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-        s1[v] *= c;
-        s2[v] *= c;
-    }
-}
-
 // Scores and dP of a tile (rows: keys) become the gradients of the logits, in place; returns the lane's sum of e2 dP.
 // For lambda, bf16 tensors add these up, tile by tile (one sum over 2 048 products was off four times as far): their D2 holds the rounding of P2 V's
 // weights and rows, which shows in a sum of so many signs.  fp32 tensors add up D2 (diff_attn_dq_f32_kernel).
-__device__ inline float diff_logit_grads(f32x16 &s1, f32x16 &s2, const f32x16 &dp, const DiffRowGrad &r, float c) {
+__device__ inline float diff_logit_grads(f32x16 &s1, f32x16 &s2, const f32x16 &dp, const DiffRowGrad &r, float c, bool far) {
     float sum = 0.f;
+    if (far) {  // in place: without the branch's two outcomes side by side in registers
+        const DiffScaling to1(c, diff_far(r.minus_m1)), to2(c, diff_far(r.minus_m2));
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            s1[v] *= to1.first;
+            s2[v] *= to2.first;
+        }
+    }
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
-        const float e1 = __builtin_amdgcn_exp2f(fmaf(s1[v], c, r.minus_m1)), e2 = __builtin_amdgcn_exp2f(fmaf(s2[v], c, r.minus_m2));
+        const float e1 = __builtin_amdgcn_exp2f(fmaf(s1[v], r.c1, r.minus_m1)), e2 = __builtin_amdgcn_exp2f(fmaf(s2[v], r.c2, r.minus_m2));
         sum = fmaf(e2, dp[v], sum);
         s1[v] = e1 * fmaf(dp[v], r.f1, r.h1);
         s2[v] = e2 * fmaf(dp[v], r.f2, r.h2);
@@ -261,7 +259,8 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dq_bf16_kernel(DiffArgs a) {
     for (int ks = 0; ks < 2 * KS; ++ks) asm volatile("" : "+v"(q[ks]), "+v"(go[ks]));  // (waited for here, not inside the loop)
     asm volatile("" : "+v"(r.minus_m1), "+v"(r.minus_m2), "+v"(r.f1), "+v"(r.h1), "+v"(r.f2), "+v"(r.h2), "+v"(r.inv2));
     const bool far = __builtin_amdgcn_ballot_w64(diff_far(r.minus_m1) || diff_far(r.minus_m2)) != 0;
-    const float scaled = far ? 1.f : a.c;
+    r.c1 = DiffScaling(a.c, diff_far(r.minus_m1)).then;
+    r.c2 = DiffScaling(a.c, diff_far(r.minus_m2)).then;
     f32x16 acc[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) diff_zero(acc[cb]);
@@ -300,8 +299,7 @@ __global__ void __launch_bounds__(256, 2) diff_attn_dq_bf16_kernel(DiffArgs a) {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) dp = mfma32(as_bf16x8(y[ks]), go[KS + ks], dp);
         if ((tile + 1) * kDiffTile > p.least) diff_hide_keys(s1, s2, tile * kDiffTile, p.limit > 0 ? p.limit : a.n_k + kDiffTile, g);
-        if (far) diff_scale_scores(s1, s2, a.c);
-        lam_sum += diff_logit_grads(s1, s2, dp, r, scaled);
+        lam_sum += diff_logit_grads(s1, s2, dp, r, a.c, far);
         bf16x8 ds1[2], ds2[2];
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
@@ -363,7 +361,8 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dq_f32_kernel(DiffArgs a) {
         asm volatile("" : "+v"(q[ks].x[0]), "+v"(q[ks].x[1]), "+v"(q[ks].x[2]), "+v"(go[ks].x[0]), "+v"(go[ks].x[1]), "+v"(go[ks].x[2]));
     asm volatile("" : "+v"(r.minus_m1), "+v"(r.minus_m2), "+v"(r.f1), "+v"(r.h1), "+v"(r.f2), "+v"(r.h2), "+v"(r.d2));
     const bool far = __builtin_amdgcn_ballot_w64(diff_far(r.minus_m1) || diff_far(r.minus_m2)) != 0;
-    const float scaled = far ? 1.f : a.c;
+    r.c1 = DiffScaling(a.c, diff_far(r.minus_m1)).then;
+    r.c2 = DiffScaling(a.c, diff_far(r.minus_m2)).then;
     f32x16 acc[CB];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) diff_zero(acc[cb]);
@@ -398,8 +397,7 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dq_f32_kernel(DiffArgs a) {
         diff_read_cols3<W, 0, 0>(v[0], cols, 0);
         __builtin_amdgcn_sched_barrier(0);
         if ((tile + 1) * kDiffTile > p.least) diff_hide_keys(s1, s2, tile * kDiffTile, p.limit > 0 ? p.limit : a.n_k + kDiffTile, g);
-        if (far) diff_scale_scores(s1, s2, a.c);
-        diff_logit_grads(s1, s2, dp, r, scaled);
+        diff_logit_grads(s1, s2, dp, r, a.c, far);
         diff_landed(v[0]);
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
@@ -759,7 +757,7 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
         if (!LAST && at + 1 < p.to) issue(stage ^ 1);
         const unsigned rows = rows0 + stage * STAGE, cols = cols0 + stage * STAGE, stats = stats0 + stage * STAGE;
         f32x16 s1, s2, dp;
-        bool far;  // a reference of the tile's queries, the first two rows of statistics, one a lane
+        bool far;  // any of the references of the tile's queries, the first two rows of statistics: all of its products are rounded then (DiffScaling)
         diff_zero(s1);
         diff_zero(s2);
         diff_zero(dp);
@@ -800,8 +798,14 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
         }
         if (LAST && at + 1 < p.to) issue(stage ^ 1);  // (not in front of the products above: two operands of theirs come from scratch memory, for which they would wait for the tile too)
         if (p.masked(a, tile)) p.hide(a, s1, s2, tile, g);
-        if (far) diff_scale_scores(s1, s2, a.c);
-        const float scaled = far ? 1.f : a.c;
+        const DiffScaling scaling(a.c, far);
+        if (far) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                s1[v] *= scaling.first;
+                s2[v] *= scaling.first;
+            }
+        }
         // four rows' statistics at a time, the next four's on their way
         {
             u32x4 st[2][6];
@@ -824,7 +828,7 @@ __global__ void __launch_bounds__(256, 1) diff_attn_dkv_f32_kernel(DiffArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int r = 4 * q4 + e;
-                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s1[r], scaled, y[0][e])), e2 = __builtin_amdgcn_exp2f(fmaf(s2[r], scaled, y[1][e]));
+                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s1[r], scaling.then, y[0][e])), e2 = __builtin_amdgcn_exp2f(fmaf(s2[r], scaling.then, y[1][e]));
                     s1[r] = e1 * fmaf(dp[r], y[2][e], y[3][e]);
                     s2[r] = e2 * fmaf(dp[r], y[4][e], y[5][e]);
                     dp[r] = fmaf(e2, y[4][e], e1 * y[2][e]);
